@@ -25,6 +25,11 @@
  *
  * tc_check_index checks an index array on the device before it is trusted.
  *
+ * For models that let a bag's rows attend to one another instead of summing
+ * them: tc_attn_forward and tc_attn_backward (with a learned bias by
+ * distance and its gradient), and for serving tc_cache_write, tc_cache_read
+ * and tc_attn_paged (a paged cache of keys and values, optionally in 8 bits).
+ *
  * Conventions shared by every call
  * --------------------------------
  * Pointers are DEVICE pointers owned by the caller unless a comment says
@@ -383,6 +388,173 @@ tc_status tc_check_index(const int64_t *table_row_offset, int32_t num_tables,
                          int32_t bags_per_table, int64_t total_rows, int64_t max_table_rows,
                          const int32_t *indices, const int32_t *bag_offsets, int64_t num_pairs,
                          int64_t *report, hipStream_t stream);
+
+/*
+ * Attention over the rows of ragged bags
+ * --------------------------------------
+ * A model that does not pool a bag's rows by a sum lets them attend to one
+ * another: bag b (a "sequence" here) has queries q_offsets[b] ..
+ * q_offsets[b+1]-1 and keys k_offsets[b] .. k_offsets[b+1]-1, so the offsets
+ * are the document mask. The queries are the last rows of their sequence:
+ * query i of b stands at position pos = i + (keys of b) - (queries of b).
+ * With query head h, key head h / (num_heads / num_kv_heads), keys j:
+ *   x      = scale * <q_i, k_j>
+ *   c      = cap * tanh(x / cap)        (cap = 0: c = x)
+ *   s      = c + bias_table[bucket_of[clamp(j - pos, -reach, reach) + reach], h]
+ *   out_i  = sum_j p_j v_j,  p = softmax of s over the visible j
+ * All j are visible, or with `causal` those with j <= pos or j <
+ * prefix_lens[b]. A query that sees no key gives a row of zeros (and -inf as
+ * its log-sum); values at keys that a query does not see, NaN and infinities
+ * too, do not enter its results.
+ *
+ * The bias is learned: bias_table is an embedding table of num_buckets rows
+ * of num_heads floats, looked up by distance, and tc_attn_backward returns
+ * its coalesced gradient, which tc_sparse_update or a dense step applies.
+ *
+ * Types: TC_F32 (products on fp32 matrix instructions) and TC_BF16 (products
+ * of bf16 values, sums in fp32; probabilities and their gradients are rounded
+ * to bf16 where they enter a product). Softmax statistics, the bias, its
+ * gradient and every sum are fp32 in both. Sums are split by sizes known to
+ * the host only, never by atomics: results repeat bit for bit.
+ *
+ * Layout: rows are found by strides in elements (tc_rows), so one array
+ * may hold q, k and v side by side, or heads may be outermost. The head_dim
+ * elements of a row are contiguous, head_dim is a multiple of 8 in [8, 128],
+ * every row starts at a multiple of 16 bytes (TC_ERR_UNSUPPORTED otherwise;
+ * 8-bit caches: of 8 bytes). Arrays may be larger than 2^31 elements.
+ */
+typedef enum tc_dtype {
+    TC_F32 = 0,
+    TC_BF16 = 1,
+    TC_FP8 = 2  /* caches only: e4m3 values, a power-of-two scale per row */
+} tc_dtype;
+
+/* Rows [token][head] of head_dim elements; strides in elements, >= 0. */
+typedef struct tc_rows {
+    void *data;
+    int64_t token_stride, head_stride;
+} tc_rows;
+
+/* What the attention calls share (host struct, read during the call). */
+typedef struct tc_attn {
+    int32_t dtype;      /* tc_dtype of q, k, v and the outputs: TC_F32 or TC_BF16 */
+    int32_t num_seqs;
+    int32_t num_heads;  /* a multiple of num_kv_heads */
+    int32_t num_kv_heads;
+    int32_t head_dim;
+    int32_t causal;     /* 0 or 1 */
+    float scale;
+    float cap;          /* >= 0; 0: no cap */
+    const float *bias_table;     /* [num_buckets x num_heads], or NULL: no bias */
+    const int32_t *bucket_of;    /* [2*reach + 1], entries in [0, num_buckets) */
+    int32_t num_buckets;
+    int32_t reach;               /* in [0, 1024] */
+    const int32_t *q_offsets;    /* [num_seqs + 1], from 0 to total_q */
+    const int32_t *k_offsets;    /* [num_seqs + 1], from 0 to total_k (not for tc_attn_paged) */
+    const int32_t *prefix_lens;  /* [num_seqs], or NULL; only with causal */
+    int64_t total_q, total_k;
+    int32_t max_q, max_k;        /* upper bounds on every sequence's queries and keys */
+} tc_attn;
+
+/*
+ * Workspace bytes of tc_attn_forward, or with `paged` of tc_attn_paged, and
+ * of tc_attn_backward, for the sizes in *a (device pointers are not read);
+ * 0 when none is needed or the sizes are out of range. Host functions.
+ */
+size_t tc_attn_workspace_bytes(const tc_attn *a, int32_t paged);
+size_t tc_attn_backward_workspace_bytes(const tc_attn *a);
+
+/*
+ * Attention forward: q [total_q x num_heads], k and v [total_k x
+ * num_kv_heads], out [total_q x num_heads] written.
+ *   out_low  NULL, or [total_q x num_heads x head_dim] bf16, contiguous,
+ *            written: what rounding out to bf16 left off. Only for TC_BF16;
+ *            tc_attn_backward takes it.
+ *   lse      NULL, or [num_heads x total_q] floats, written: the natural
+ *            log of the sum of exp(s) over the visible keys
+ *   workspace device memory of tc_attn_workspace_bytes(a, 0) bytes,
+ *            256-byte aligned; no initial contents are needed
+ */
+tc_status tc_attn_forward(const tc_attn *a, tc_rows q, tc_rows k, tc_rows v, tc_rows out,
+                          void *out_low, float *lse, void *workspace, size_t workspace_bytes,
+                          hipStream_t stream);
+
+/*
+ * Attention backward: from the arguments and outputs of tc_attn_forward and
+ * the output's gradient grad_out, the gradients grad_q [total_q x num_heads],
+ * grad_k and grad_v [total_k x num_kv_heads] (summed over the heads that
+ * share a key head), all written, and
+ *   grad_bias  [num_buckets x num_heads] floats, written: the coalesced
+ *              gradient of bias_table; NULL to leave it out, and NULL
+ *              without a bias
+ *   out_low    as written by the forward, or NULL: the row sums <grad_out,
+ *              out> then carry out's rounding to bf16
+ *   workspace  tc_attn_backward_workspace_bytes(a) bytes, 256-byte aligned
+ */
+tc_status tc_attn_backward(const tc_attn *a, tc_rows q, tc_rows k, tc_rows v, tc_rows out,
+                           const void *out_low, const float *lse, tc_rows grad_out,
+                           tc_rows grad_q, tc_rows grad_k, tc_rows grad_v, float *grad_bias,
+                           void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * A paged cache of keys and values (host struct). Page p, slot s and key
+ * head h hold head_dim elements at data + p*page_stride + s*slot_stride +
+ * h*head_stride (elements, the same strides for k and v). Position j of
+ * sequence b is slot j % page_size of page page_table[b*max_pages +
+ * j / page_size]; lens[b] positions are held (never more than
+ * max_pages*page_size are touched). Page entries that hold positions must
+ * be in range, as indices of the embedding calls must; others are not read,
+ * and slots past lens[b] are never read, so they need no contents.
+ *
+ * TC_FP8: row x of one position and head is stored as e4m3 values
+ * x * 2^-e, rounded to nearest even, where e is the least integer with
+ * max|x| <= 448 * 2^e (within [-126, 127]; 0 for a zero row), and e + 127 in
+ * k_exp / v_exp, [num_pages x page_size x num_kv_heads] bytes. A row that
+ * holds a NaN or an infinity is stored as NaN throughout (exponent byte 255).
+ * Reading gives the stored value times 2^e, which bf16 and fp32 hold exactly
+ * down to bf16's least normal number 2^-126; smaller ones are rounded in
+ * bf16's subnormal range or to zero.
+ */
+typedef struct tc_cache {
+    int32_t dtype;  /* the rows' dtype, or TC_FP8 */
+    int32_t page_size;
+    int32_t num_kv_heads;
+    int32_t head_dim;
+    void *k, *v;
+    uint8_t *k_exp, *v_exp;  /* TC_FP8 only */
+    int64_t page_stride, slot_stride, head_stride;
+    const int32_t *page_table;  /* [num_seqs x max_pages] */
+    int32_t max_pages;
+    const int32_t *lens;  /* [num_seqs] */
+} tc_cache;
+
+/*
+ * Appends rows: the n = offsets[b+1] - offsets[b] rows of sequence b go to
+ * its last positions lens[b] - n .. lens[b] - 1 (rows before position 0 or
+ * past the page table are left out). k and v are [total x num_kv_heads]
+ * rows of `dtype`; offsets is [num_seqs + 1] from 0 to total. Positions must
+ * not share a slot.
+ */
+tc_status tc_cache_write(const tc_cache *c, int32_t dtype, int32_t num_seqs,
+                         const int32_t *offsets, int64_t total, tc_rows k, tc_rows v,
+                         hipStream_t stream);
+
+/* Reads the same rows back as `dtype` values (rows that tc_cache_write
+ * leaves out are written as zeros). */
+tc_status tc_cache_read(const tc_cache *c, int32_t dtype, int32_t num_seqs,
+                        const int32_t *offsets, int64_t total, tc_rows k, tc_rows v,
+                        hipStream_t stream);
+
+/*
+ * tc_attn_forward with keys and values from a cache that already holds the
+ * queries' own rows: sequence b has lens[b] keys and its queries are the last
+ * ones of them (one query per sequence: a decoding step). a->k_offsets and
+ * a->total_k are not used; a->max_k bounds lens. a->dtype is the type of q
+ * and out. The workspace is tc_attn_workspace_bytes(a, 1) bytes, 256-byte
+ * aligned.
+ */
+tc_status tc_attn_paged(const tc_attn *a, tc_rows q, const tc_cache *c, tc_rows out, float *lse,
+                        void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Static text for a status code. */
 const char *tc_status_string(tc_status status);

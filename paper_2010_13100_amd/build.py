@@ -39,7 +39,8 @@ SAN_FLAGS = ["-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsaniti
 
 LIBS = {
     "libtc.so": ["tc_api.hip", "tc_gather_reduce.hip", "tc_backward.hip", "tc_cast.hip",
-                 "tc_update.hip", "tc_check.hip"],
+                 "tc_update.hip", "tc_check.hip", "tc_attn_forward.hip",
+                 "tc_attn_backward.hip", "tc_cache.hip"],
     "libtc_workload.so": ["workload_fill.hip"],
 }
 

@@ -1,0 +1,316 @@
+// Shared parts of the attention kernels: element types, matrix products,
+// where rows lie, and the score.
+//
+// Notation: b sequence, i query, j key, h query head, z = <q_i, k_j>. Scores
+// are kept in units of log 2, so that exponentials are one exp2:
+//   x = c1*z                                (no cap; c1 = scale*log2 e)
+//   x = c2*tanh(scale*z/cap), c2 = cap*log2 e
+//       = c2*(1 - 2/(1 + exp2(c1*z)))       (c1 = 2*scale*log2 e/cap)
+//   s = x + log2 e * bias
+// The keys that query i sees are j < lim_i, with lim_i = keys (no mask) or
+// max(pos_i + 1, prefix) cut to [0, keys]: a run from 0 that grows with i.
+#pragma once
+
+#include "tc_internal.h"
+
+namespace tc {
+namespace attn {
+
+typedef __bf16 bf16;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct fp8 {
+    uint8_t bits;  // e4m3
+};
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kMaxHeadDim = 128;
+constexpr int kMaxReach = 1024;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What every kernel of a call needs. Pointers as in tc_attn.
+struct Args {
+    int32_t num_seqs, heads, kv_heads, group, dim;
+    int32_t causal, capped, reach;
+    float scale, c1, c2;
+    const float *table;  // nullptr: no bias
+    const int32_t *bucket_of;
+    const int32_t *q_off, *k_off, *prefix;
+    int64_t total_q;
+};
+
+inline Args make_args(const tc_attn &a) {
+    Args r{};
+    r.num_seqs = a.num_seqs;
+    r.heads = a.num_heads;
+    r.kv_heads = a.num_kv_heads;
+    r.group = a.num_heads / a.num_kv_heads;
+    r.dim = a.head_dim;
+    r.causal = a.causal;
+    r.capped = a.cap > 0.0f;
+    r.reach = a.reach;
+    r.scale = a.scale;
+    r.c1 = r.capped ? 2.0f * a.scale * kLog2e / a.cap : a.scale * kLog2e;
+    r.c2 = a.cap * kLog2e;
+    r.table = a.bias_table;
+    r.bucket_of = a.bucket_of;
+    r.q_off = a.q_offsets;
+    r.k_off = a.k_offsets;
+    r.prefix = a.causal ? a.prefix_lens : nullptr;
+    r.total_q = a.total_q;
+    return r;
+}
+
+// One sequence.
+struct Seq {
+    int32_t b, qn, kn, shift, prefix;  // pos_i = i + shift
+    int64_t q0, k0;                    // first query and key token
+};
+
+__device__ __forceinline__ Seq seq_of(const Args &a, int b, int kn_paged) {
+    Seq s;
+    s.b = b;
+    const int32_t q0 = a.q_off[b];
+    s.qn = a.q_off[b + 1] - q0;
+    s.q0 = q0;
+    if (kn_paged >= 0) {
+        s.kn = kn_paged;
+        s.k0 = 0;
+    } else {
+        const int32_t k0 = a.k_off[b];
+        s.kn = a.k_off[b + 1] - k0;
+        s.k0 = k0;
+    }
+    s.shift = s.kn - s.qn;
+    s.prefix = a.prefix ? a.prefix[b] : 0;
+    return s;
+}
+
+// Keys that query i sees.
+__device__ __forceinline__ int limit(const Args &a, const Seq &s, int i) {
+    if (!a.causal) return s.kn;
+    const int n = max(i + s.shift + 1, s.prefix);
+    return min(max(n, 0), s.kn);
+}
+
+// First query that sees key j (s.qn if none does).
+__device__ __forceinline__ int first_query(const Args &a, const Seq &s, int j) {
+    if (!a.causal || j < s.prefix) return 0;
+    return min(max(j - s.shift, 0), s.qn);
+}
+
+// tanh of the scaled product, from c1*z.
+__device__ __forceinline__ float tanh_of(float y) {
+    return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + exp2_fast(y)), 1.0f);
+}
+
+__device__ __forceinline__ float log2_bias(const Args &a, int h, int delta) {
+    const int d = min(max(delta, -a.reach), a.reach) + a.reach;
+    return a.table[int64_t(a.bucket_of[d]) * a.heads + h] * kLog2e;
+}
+
+// --- elements ---------------------------------------------------------------
+
+__device__ __forceinline__ float exp_scale(uint32_t e) {
+    return __builtin_bit_cast(float, e << 23);
+}
+
+__device__ __forceinline__ float load1(const float *p, uint32_t) { return *p; }
+__device__ __forceinline__ float load1(const bf16 *p, uint32_t) { return float(*p); }
+__device__ __forceinline__ float load1(const fp8 *p, uint32_t e) {
+    return __builtin_amdgcn_cvt_f32_fp8(int(p->bits), 0) * exp_scale(e);
+}
+
+template <class T>
+struct El;
+template <>
+struct El<float> {
+    typedef f32x8 v8;
+};
+template <>
+struct El<bf16> {
+    typedef bf16x8 v8;
+};
+
+// --- argument checks (tc_cache.hip, tc_attn_forward.hip) ----------------------
+
+tc_status check_rows(const char *fn, const char *name, const tc_rows &r, int32_t dtype,
+                     bool required);
+tc_status check_cache(const char *fn, const tc_cache *c, int32_t dtype);
+// The sizes and pointers of *a; `paged`: k_offsets and total_k are not used.
+tc_status check_attn(const char *fn, const tc_attn *a, bool paged);
+
+// --- where the keys lie -----------------------------------------------------
+
+struct Loc {
+    int64_t k, v;  // element offsets
+    int64_t e;     // of the exponent bytes
+};
+
+// Keys of one sequence and key head in [token][head] rows.
+template <class CT>
+struct DenseKv {
+    typedef CT type;
+    const CT *kp, *vp;
+    int64_t kts, vts;
+    __device__ __forceinline__ Loc loc(int j) const { return {j * kts, j * vts, 0}; }
+    __device__ __forceinline__ const CT *k(const Loc &l) const { return kp + l.k; }
+    __device__ __forceinline__ const CT *v(const Loc &l) const { return vp + l.v; }
+    __device__ __forceinline__ uint32_t k_exp(const Loc &) const { return 127; }
+    __device__ __forceinline__ uint32_t v_exp(const Loc &) const { return 127; }
+};
+
+// The same in pages.
+template <class CT>
+struct PagedKv {
+    typedef CT type;
+    const CT *kp, *vp;        // with the head's offset
+    const uint8_t *ke, *ve;   // with the head's offset
+    const int32_t *pages;     // of the sequence
+    int64_t page_stride, slot_stride;
+    int32_t page_size, shift, kv_heads;  // shift: log2 page_size, or -1
+    __device__ __forceinline__ Loc loc(int j) const {
+        const int p = shift >= 0 ? j >> shift : int(uint32_t(j) / uint32_t(page_size));
+        const int s = j - p * page_size;
+        const int64_t page = pages[p];
+        const int64_t o = page * page_stride + s * slot_stride;
+        return {o, o, (page * page_size + s) * kv_heads};
+    }
+    __device__ __forceinline__ const CT *k(const Loc &l) const { return kp + l.k; }
+    __device__ __forceinline__ const CT *v(const Loc &l) const { return vp + l.v; }
+    __device__ __forceinline__ uint32_t k_exp(const Loc &l) const { return ke ? ke[l.e] : 127; }
+    __device__ __forceinline__ uint32_t v_exp(const Loc &l) const { return ve ? ve[l.e] : 127; }
+};
+
+// Where a call's keys come from: dense rows, or a cache.
+struct Source {
+    tc_rows k, v;    // dense
+    tc_cache cache;  // paged
+    int32_t paged, page_shift;
+};
+
+inline Source dense_source(tc_rows k, tc_rows v) {
+    Source s{};
+    s.k = k;
+    s.v = v;
+    return s;
+}
+
+inline Source paged_source(const tc_cache &c) {
+    Source s{};
+    s.cache = c;
+    s.paged = 1;
+    s.page_shift = -1;
+    for (int b = 0; b < 31; b++)
+        if ((1 << b) == c.page_size) s.page_shift = b;
+    return s;
+}
+
+// Positions that sequence b's cache holds.
+__device__ __forceinline__ int cache_len(const tc_cache &c, int b) {
+    const int64_t cap = int64_t(c.max_pages) * c.page_size;
+    const int n = c.lens[b] < 0 ? 0 : c.lens[b];
+    return n < cap ? n : int(cap);
+}
+
+template <class CT, bool PAGED>
+struct KvOf;
+template <class CT>
+struct KvOf<CT, false> {
+    typedef DenseKv<CT> type;
+    static __device__ __forceinline__ type make(const Source &s, const Seq &q, int kvh) {
+        return {static_cast<const CT *>(s.k.data) + q.k0 * s.k.token_stride + kvh * s.k.head_stride,
+                static_cast<const CT *>(s.v.data) + q.k0 * s.v.token_stride + kvh * s.v.head_stride,
+                s.k.token_stride, s.v.token_stride};
+    }
+};
+template <class CT>
+struct KvOf<CT, true> {
+    typedef PagedKv<CT> type;
+    static __device__ __forceinline__ type make(const Source &s, const Seq &q, int kvh) {
+        const tc_cache &c = s.cache;
+        return {static_cast<const CT *>(c.k) + kvh * c.head_stride,
+                static_cast<const CT *>(c.v) + kvh * c.head_stride,
+                c.k_exp ? c.k_exp + kvh : nullptr,
+                c.v_exp ? c.v_exp + kvh : nullptr,
+                c.page_table + int64_t(q.b) * c.max_pages,
+                c.page_stride,
+                c.slot_stride,
+                c.page_size,
+                s.page_shift,
+                c.num_kv_heads};
+    }
+};
+
+template <bool PAGED>
+__device__ __forceinline__ Seq seq_at(const Args &a, const Source &s, int b) {
+    return seq_of(a, b, PAGED ? cache_len(s.cache, b) : -1);
+}
+
+// --- one row by one wavefront -----------------------------------------------
+//
+// The formulas taken literally: a lane holds elements lane and lane + 64 of a
+// row. Only keys (queries) that the mask leaves are read.
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
+    return x;
+}
+
+struct Row2 {
+    float a, b;
+};
+
+template <class CT>
+__device__ __forceinline__ Row2 load_row(const CT *p, uint32_t e, int dim) {
+    const int l = threadIdx.x & (kWave - 1);
+    return {l < dim ? load1(p + l, e) : 0.0f, l + 64 < dim ? load1(p + l + 64, e) : 0.0f};
+}
+
+template <class T>
+__device__ __forceinline__ void store_row(T *p, Row2 r, int dim) {
+    const int l = threadIdx.x & (kWave - 1);
+    if (l < dim) p[l] = T(r.a);
+    if (l + 64 < dim) p[l + 64] = T(r.b);
+}
+
+__device__ __forceinline__ float dot(Row2 x, Row2 y) { return wave_sum(x.a * y.a + x.b * y.b); }
+
+struct RowState {
+    float m, l;  // running maximum of s, sum of exp2(s - m)
+    Row2 o;
+};
+
+// Keys [j0, j1) of one query into st.
+template <class KV>
+__device__ void row_forward(const Args &a, const KV &kv, Row2 q, int h, int pos, int j0, int j1,
+                            RowState &st) {
+    for (int j = j0; j < j1; j++) {
+        const Loc l = kv.loc(j);
+        const float z = dot(q, load_row(kv.k(l), kv.k_exp(l), a.dim));
+        float s = a.capped ? a.c2 * tanh_of(a.c1 * z) : a.c1 * z;
+        if (a.table) s += log2_bias(a, h, j - pos);
+        const float m = fmaxf(st.m, s), base = m == -INFINITY ? 0.0f : m;
+        const float keep = exp2_fast(st.m - base), p = exp2_fast(s - base);
+        const Row2 v = load_row(kv.v(l), kv.v_exp(l), a.dim);
+        st.m = m;
+        st.l = st.l * keep + p;
+        st.o.a = st.o.a * keep + p * v.a;
+        st.o.b = st.o.b * keep + p * v.b;
+    }
+}
+
+}  // namespace attn
+}  // namespace tc

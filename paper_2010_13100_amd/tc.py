@@ -18,11 +18,39 @@ TC_OK, TC_ERR_INVALID_ARG, TC_ERR_UNSUPPORTED, TC_ERR_WORKSPACE, TC_ERR_HIP = ra
 TC_NOALLOC_SCRATCH_BYTES = 16 << 20
 TC_INDEX_OK, TC_INDEX_BAD_TABLE_OFFSETS, TC_INDEX_BAD_BAG_OFFSETS, TC_INDEX_OUT_OF_RANGE = range(4)
 TC_OPT_SGD, TC_OPT_ADAGRAD, TC_OPT_RMSPROP, TC_OPT_ROWWISE_ADAGRAD = range(4)
+TC_F32, TC_BF16, TC_FP8 = range(3)
+DTYPES = {torch.float32: TC_F32, torch.bfloat16: TC_BF16, torch.float8_e4m3fn: TC_FP8,
+          torch.uint8: TC_FP8}
 OPTIMIZERS = {"sgd": TC_OPT_SGD, "adagrad": TC_OPT_ADAGRAD, "rmsprop": TC_OPT_RMSPROP,
               "rowwise_adagrad": TC_OPT_ROWWISE_ADAGRAD}
 
 _vp, _i32, _i64, _f32, _sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
                               ctypes.c_size_t)
+
+
+class TcRows(ctypes.Structure):
+    """tc_rows"""
+    _fields_ = [("data", _vp), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class TcAttn(ctypes.Structure):
+    """tc_attn"""
+    _fields_ = [("dtype", _i32), ("num_seqs", _i32), ("num_heads", _i32), ("num_kv_heads", _i32),
+                ("head_dim", _i32), ("causal", _i32), ("scale", _f32), ("cap", _f32),
+                ("bias_table", _vp), ("bucket_of", _vp), ("num_buckets", _i32), ("reach", _i32),
+                ("q_offsets", _vp), ("k_offsets", _vp), ("prefix_lens", _vp), ("total_q", _i64),
+                ("total_k", _i64), ("max_q", _i32), ("max_k", _i32)]
+
+
+class TcCache(ctypes.Structure):
+    """tc_cache"""
+    _fields_ = [("dtype", _i32), ("page_size", _i32), ("num_kv_heads", _i32), ("head_dim", _i32),
+                ("k", _vp), ("v", _vp), ("k_exp", _vp), ("v_exp", _vp), ("page_stride", _i64),
+                ("slot_stride", _i64), ("head_stride", _i64), ("page_table", _vp),
+                ("max_pages", _i32), ("lens", _vp)]
+
+
+_attn_p, _cache_p = ctypes.POINTER(TcAttn), ctypes.POINTER(TcCache)
 
 _SIGNATURES = {
     "tc_embed_forward": (_i32, [_vp, _i64, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _vp]),
@@ -45,6 +73,14 @@ _SIGNATURES = {
     "tc_embed_expand": (_i32, [_vp, _i32, _i32, _vp, _i64, _vp, _vp]),
     "tc_embed_coalesce": (_i32, [_vp, _i64, _i32, _vp, _vp, _vp, _i64, _vp, _vp, _sz, _vp]),
     "tc_check_index": (_i32, [_vp, _i32, _i32, _i64, _i64, _vp, _vp, _i64, _vp, _vp]),
+    "tc_attn_workspace_bytes": (_sz, [_attn_p, _i32]),
+    "tc_attn_backward_workspace_bytes": (_sz, [_attn_p]),
+    "tc_attn_forward": (_i32, [_attn_p, TcRows, TcRows, TcRows, TcRows, _vp, _vp, _vp, _sz, _vp]),
+    "tc_attn_backward": (_i32, [_attn_p, TcRows, TcRows, TcRows, TcRows, _vp, _vp, TcRows, TcRows,
+                                TcRows, TcRows, _vp, _vp, _sz, _vp]),
+    "tc_attn_paged": (_i32, [_attn_p, TcRows, _cache_p, TcRows, _vp, _vp, _sz, _vp]),
+    "tc_cache_write": (_i32, [_cache_p, _i32, _i32, _vp, _i64, TcRows, TcRows, _vp]),
+    "tc_cache_read": (_i32, [_cache_p, _i32, _i32, _vp, _i64, TcRows, TcRows, _vp]),
     "tc_status_string": (ctypes.c_char_p, [_i32]),
     "tc_last_error": (ctypes.c_char_p, []),
     "tc_abi_version": (_i32, []),
@@ -244,6 +280,283 @@ def tc_embed_coalesce(expanded, num_pairs, seg_offsets, sorted_pos, num_unique, 
         _ptr(num_unique, torch.int32, "num_unique"), max_unique,
         _ptr(coal_grad, torch.float32, "coal_grad"), *_ws(workspace), _stream(stream)),
         "tc_embed_coalesce")
+
+
+def _rows(t: torch.Tensor | None, dtype, name, heads, dim) -> TcRows:
+    """tc_rows of a [tokens, heads, dim] tensor whose last dimension is contiguous."""
+    if t is None:
+        return TcRows(None, 0, 0)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"{name} must be [tokens, {heads}, {dim}], got {list(t.shape)}")
+    st = t.stride()
+    if st[2] != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return TcRows(t.data_ptr(), st[0] if t.shape[0] > 1 else 0, st[1] if heads > 1 else 0)
+
+
+def _same_tokens(what, first, *others):
+    for name, t in others:
+        if t is not None and t.shape[0] != first:
+            raise ValueError(f"{what}: {name} has {t.shape[0]} tokens, not {first}")
+
+
+def tc_attn_workspace_bytes(attn: TcAttn, paged: bool) -> int:
+    return int(_lib.tc_attn_workspace_bytes(attn, int(paged)))
+
+
+def tc_attn_backward_workspace_bytes(attn: TcAttn) -> int:
+    return int(_lib.tc_attn_backward_workspace_bytes(attn))
+
+
+def tc_attn_forward(attn: TcAttn, q, k, v, out, out_low=None, lse=None, workspace=None,
+                    stream=None) -> None:
+    dt, h, kv, d = _attn_layout(attn)
+    _same_tokens("tc_attn_forward", attn.total_q, ("q", q), ("out", out))
+    _same_tokens("tc_attn_forward", attn.total_k, ("k", k), ("v", v))
+    _check(_lib.tc_attn_forward(
+        attn, _rows(q, dt, "q", h, d), _rows(k, dt, "k", kv, d), _rows(v, dt, "v", kv, d),
+        _rows(out, dt, "out", h, d), _sized(out_low, torch.bfloat16, "out_low",
+                                            attn.total_q * h * d),
+        _sized(lse, torch.float32, "lse", h * attn.total_q), *_ws(workspace), _stream(stream)),
+        "tc_attn_forward")
+
+
+def tc_attn_backward(attn: TcAttn, q, k, v, out, out_low, lse, grad_out, grad_q, grad_k, grad_v,
+                     grad_bias=None, workspace=None, stream=None) -> None:
+    dt, h, kv, d = _attn_layout(attn)
+    _same_tokens("tc_attn_backward", attn.total_q, ("q", q), ("out", out),
+                 ("grad_out", grad_out), ("grad_q", grad_q))
+    _same_tokens("tc_attn_backward", attn.total_k, ("k", k), ("v", v), ("grad_k", grad_k),
+                 ("grad_v", grad_v))
+    _check(_lib.tc_attn_backward(
+        attn, _rows(q, dt, "q", h, d), _rows(k, dt, "k", kv, d), _rows(v, dt, "v", kv, d),
+        _rows(out, dt, "out", h, d), _sized(out_low, torch.bfloat16, "out_low",
+                                            attn.total_q * h * d),
+        _sized(lse, torch.float32, "lse", h * attn.total_q),
+        _rows(grad_out, dt, "grad_out", h, d), _rows(grad_q, dt, "grad_q", h, d),
+        _rows(grad_k, dt, "grad_k", kv, d), _rows(grad_v, dt, "grad_v", kv, d),
+        _sized(grad_bias, torch.float32, "grad_bias", attn.num_buckets * h), *_ws(workspace),
+        _stream(stream)), "tc_attn_backward")
+
+
+def tc_attn_paged(attn: TcAttn, q, cache: TcCache, out, lse=None, workspace=None,
+                  stream=None) -> None:
+    dt, h, _, d = _attn_layout(attn)
+    _same_tokens("tc_attn_paged", attn.total_q, ("q", q), ("out", out))
+    _check(_lib.tc_attn_paged(
+        attn, _rows(q, dt, "q", h, d), cache, _rows(out, dt, "out", h, d),
+        _sized(lse, torch.float32, "lse", h * attn.total_q), *_ws(workspace), _stream(stream)),
+        "tc_attn_paged")
+
+
+def tc_cache_write(cache: TcCache, num_seqs, offsets, k, v, stream=None) -> None:
+    _cache_rows(_lib.tc_cache_write, "tc_cache_write", cache, num_seqs, offsets, k, v, stream)
+
+
+def tc_cache_read(cache: TcCache, num_seqs, offsets, k, v, stream=None) -> None:
+    _cache_rows(_lib.tc_cache_read, "tc_cache_read", cache, num_seqs, offsets, k, v, stream)
+
+
+def _cache_rows(fn, name, cache, num_seqs, offsets, k, v, stream):
+    h, d = cache.num_kv_heads, cache.head_dim
+    if k.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"k must be float32 or bfloat16, got {k.dtype}")
+    _same_tokens(name, k.shape[0], ("v", v))
+    _check(fn(cache, DTYPES[k.dtype], num_seqs, _sized(offsets, torch.int32, "offsets",
+                                                       num_seqs + 1), k.shape[0],
+              _rows(k, k.dtype, "k", h, d), _rows(v, k.dtype, "v", h, d), _stream(stream)), name)
+
+
+def _sized(t, dtype, name, numel):
+    """_ptr of a tensor that holds at least `numel` elements."""
+    if t is not None and t.numel() < numel:
+        raise ValueError(f"{name} holds {t.numel()} elements, needs {numel}")
+    return _ptr(t, dtype, name)
+
+
+_TORCH_TYPES = {TC_F32: torch.float32, TC_BF16: torch.bfloat16}
+
+
+def _attn_layout(attn: TcAttn):
+    return (_TORCH_TYPES.get(attn.dtype), attn.num_heads, attn.num_kv_heads, attn.head_dim)
+
+
+def relative_buckets(num_buckets: int, reach: int, both_sides: bool = False) -> torch.Tensor:
+    """bucket_of for distances -reach .. reach (host int32, [2*reach + 1]):
+    the nearest distances have a bucket each, farther ones share buckets that
+    grow by one ratio up to `reach`, from where on all share the last. Without
+    both_sides the keys after the query fall into the bucket of distance 0;
+    with it half the buckets are theirs. Exact (integer arithmetic)."""
+    if num_buckets < 1 or reach < 0 or (both_sides and num_buckets % 2):
+        raise ValueError("relative_buckets: num_buckets must be positive, and even with "
+                         "both_sides; reach must not be negative")
+    side = num_buckets // 2 if both_sides else num_buckets
+    near = max(side // 2, 1)
+    far = side - near
+    # bucket near + b (b >= 1) starts at the least n with (n/near)^far >= (reach/near)^b
+    starts = []
+    n = near
+    for b in range(1, far):
+        while n < reach and n ** far * near ** b < reach ** b * near ** far:
+            n += 1
+        starts.append(n)
+
+    def one(n):
+        return n if n < near else min(near + sum(n >= s for s in starts), side - 1)
+
+    out = [(one(-d) if d <= 0 else (side + one(d) if both_sides else 0))
+           for d in range(-reach, reach + 1)]
+    return torch.tensor(out, dtype=torch.int32)
+
+
+class PagedCache:
+    """A paged cache of keys and values: [num_pages, page_size, num_kv_heads,
+    head_dim] tensors, or views of such (the last dimension contiguous, k and
+    v alike), in float32, bfloat16 or 8 bits (float8_e4m3fn or uint8, with
+    exponent bytes [num_pages, page_size, num_kv_heads]). The calls take the
+    page table ([num_seqs, max_pages] int32) and the lengths the cache has
+    after the new rows ([num_seqs] int32), both on the GPU."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        if k.dtype not in DTYPES or v.dtype != k.dtype:
+            raise ValueError(f"cache: unsupported dtypes {k.dtype}, {v.dtype}")
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride():
+            raise ValueError("cache: k and v must be [pages, page_size, heads, dim], laid out alike")
+        if k.stride(3) != 1:
+            raise ValueError("cache: the last dimension must be contiguous")
+        self.quantised = DTYPES[k.dtype] == TC_FP8
+        if self.quantised != (k_exp is not None) or self.quantised != (v_exp is not None):
+            raise ValueError("cache: exponent bytes go with an 8-bit cache")
+        for e in (k_exp, v_exp):
+            if e is not None and (e.dtype != torch.uint8 or e.shape != k.shape[:3]):
+                raise ValueError("cache: exponents must be uint8 [pages, page_size, heads]")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+
+    @classmethod
+    def empty(cls, num_pages, page_size, num_kv_heads, head_dim, dtype=torch.float8_e4m3fn,
+              device="cuda"):
+        shape = (num_pages, page_size, num_kv_heads, head_dim)
+        exps = [torch.empty(shape[:3], dtype=torch.uint8, device=device) if DTYPES[dtype] == TC_FP8
+                else None for _ in range(2)]
+        return cls(torch.empty(shape, dtype=dtype, device=device),
+                   torch.empty(shape, dtype=dtype, device=device), *exps)
+
+    def struct(self, page_table, lens) -> TcCache:
+        k = self.k
+        if not k.is_cuda or not self.v.is_cuda:
+            raise ValueError("cache must be on the GPU")
+        if page_table.dim() != 2 or page_table.shape[0] != lens.numel():
+            raise ValueError("page_table must be [num_seqs, max_pages], lens [num_seqs]")
+        return TcCache(DTYPES[k.dtype], k.shape[1], k.shape[2], k.shape[3], k.data_ptr(),
+                       self.v.data_ptr(), _ptr(self.k_exp, torch.uint8, "k_exp"),
+                       _ptr(self.v_exp, torch.uint8, "v_exp"), k.stride(0), k.stride(1),
+                       k.stride(2), _ptr(page_table, torch.int32, "page_table"),
+                       page_table.shape[1], _ptr(lens, torch.int32, "lens"))
+
+    def write(self, k, v, offsets, page_table, lens, stream=None):
+        """Appends the rows k, v ([tokens, heads, dim]) of every sequence to
+        its last positions."""
+        tc_cache_write(self.struct(page_table, lens), lens.numel(), offsets, k, v, stream)
+
+    def read(self, k, v, offsets, page_table, lens, stream=None):
+        """Reads the last rows of every sequence into k and v."""
+        tc_cache_read(self.struct(page_table, lens), lens.numel(), offsets, k, v, stream)
+
+
+class BagAttention:
+    """Device buffers for attention over one shape of ragged bags, and its
+    calls: forward, backward (train=True) and, over a PagedCache,
+    forward_paged (paged=True). Outputs are the attributes out, lse, dq, dk,
+    dv and grad_bias.
+
+    total_q, total_k: tokens of the queries and keys (by default all
+    sequences are full); max_q, max_k: upper bounds on a sequence's queries
+    and keys. bias_table [num_buckets, num_heads] float32 and bucket_of
+    [2*reach + 1] int32 (see relative_buckets) give the distance bias."""
+
+    def __init__(self, *, num_seqs: int, num_heads: int, head_dim: int, max_q: int,
+                 max_k: int | None = None, total_q: int | None = None,
+                 total_k: int | None = None, num_kv_heads: int | None = None,
+                 dtype=torch.bfloat16, causal: bool = False, scale: float | None = None,
+                 cap: float = 0.0, bias_table=None, bucket_of=None, train: bool = False,
+                 paged: bool = False, device="cuda"):
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"BagAttention: dtype must be float32 or bfloat16, got {dtype}")
+        if train and paged:
+            raise ValueError("BagAttention: a paged cache is for serving, not for training")
+        if (bias_table is None) != (bucket_of is None):
+            raise ValueError("BagAttention: bias_table and bucket_of go together")
+        kv = num_heads if num_kv_heads is None else num_kv_heads
+        max_k = max_q if max_k is None else max_k
+        total_q = num_seqs * max_q if total_q is None else total_q
+        total_k = (0 if paged else num_seqs * max_k) if total_k is None else total_k
+        self.bias_table, self.bucket_of = bias_table, bucket_of
+        buckets = reach = 0
+        if bias_table is not None:
+            buckets, reach = bias_table.shape[0], (bucket_of.numel() - 1) // 2
+            if bias_table.shape[1] != num_heads or bucket_of.numel() % 2 == 0:
+                raise ValueError("BagAttention: bias_table must be [num_buckets, num_heads], "
+                                 "bucket_of [2*reach + 1]")
+        self.attn = TcAttn(
+            DTYPES[dtype], num_seqs, num_heads, kv, head_dim, int(causal),
+            head_dim ** -0.5 if scale is None else scale, cap,
+            _ptr(bias_table, torch.float32, "bias_table"),
+            _ptr(bucket_of, torch.int32, "bucket_of"), buckets, reach, None, None, None, total_q,
+            total_k, max_q, max_k)
+        new = dict(dtype=dtype, device=device)
+        self.out = torch.empty((total_q, num_heads, head_dim), **new)
+        ws = tc_attn_workspace_bytes(self.attn, paged)
+        self.lse = self.out_low = self.grad_bias = None
+        if train:
+            self.lse = torch.empty((num_heads, total_q), dtype=torch.float32, device=device)
+            if dtype == torch.bfloat16:
+                self.out_low = torch.empty_like(self.out)
+            self.dq = torch.empty_like(self.out)
+            self.dk = torch.empty((total_k, kv, head_dim), **new)
+            self.dv = torch.empty_like(self.dk)
+            if bias_table is not None:
+                self.grad_bias = torch.empty_like(bias_table)
+            ws = max(ws, tc_attn_backward_workspace_bytes(self.attn))
+        self.workspace = torch.empty(ws, dtype=torch.uint8, device=device) if ws else None
+
+    def _bind(self, q_offsets, k_offsets, prefix_lens) -> TcAttn:
+        a, n = self.attn, self.attn.num_seqs
+        a.q_offsets = _sized(q_offsets, torch.int32, "q_offsets", n + 1)
+        a.k_offsets = _sized(k_offsets, torch.int32, "k_offsets", n + 1)
+        a.prefix_lens = _sized(prefix_lens, torch.int32, "prefix_lens", n)
+        return a
+
+    def forward(self, q, k, v, q_offsets, k_offsets=None, prefix_lens=None, stream=None):
+        """Attention of q over k, v ([tokens, heads, dim]; k_offsets defaults
+        to q_offsets) into self.out."""
+        a = self._bind(q_offsets, q_offsets if k_offsets is None else k_offsets, prefix_lens)
+        tc_attn_forward(a, q, k, v, self.out, self.out_low, self.lse, self.workspace, stream)
+        return self.out
+
+    def backward(self, q, k, v, grad_out, q_offsets, k_offsets=None, prefix_lens=None,
+                 stream=None):
+        """Gradients of the last forward's inputs into self.dq, dk, dv and
+        grad_bias."""
+        if self.lse is None:
+            raise ValueError("BagAttention.backward needs train=True")
+        a = self._bind(q_offsets, q_offsets if k_offsets is None else k_offsets, prefix_lens)
+        tc_attn_backward(a, q, k, v, self.out, self.out_low, self.lse, grad_out, self.dq, self.dk,
+                         self.dv, self.grad_bias, self.workspace, stream)
+
+    def forward_paged(self, q, cache: PagedCache, q_offsets, page_table, lens, prefix_lens=None,
+                      stream=None):
+        """Attention of the newest rows q over a cache that holds them already
+        into self.out."""
+        a = self._bind(q_offsets, None, prefix_lens)
+        if lens.numel() != a.num_seqs:
+            raise ValueError(f"lens holds {lens.numel()} sequences, not {a.num_seqs}")
+        tc_attn_paged(a, q, cache.struct(page_table, lens), self.out, self.lse, self.workspace,
+                      stream)
+        return self.out
 
 
 class EmbeddingTrainer:
