@@ -1,42 +1,641 @@
 // Attention forward over ragged bags (tc_attn_forward) and over a paged cache
 // (tc_attn_paged).
-#include "tc_attn.h"
+#include "tc_attn_tile.h"
 
 namespace tc {
 namespace {
 
 using namespace attn;
 
-// One wavefront per (query, head).
-template <class T, class CT, bool PAGED>
-__global__ __launch_bounds__(kWave) void k_attn_rows(Args a, Source src, tc_rows q, tc_rows out,
-                                                     bf16 *out_low, float *lse) {
-    const int i = blockIdx.x, h = blockIdx.y;
-    const Seq s = seq_at<PAGED>(a, src, blockIdx.z);
-    if (i >= s.qn) return;
-    const auto kv = KvOf<CT, PAGED>::make(src, s, h / a.group);
-    const int64_t t = s.q0 + i;
-    RowState st{-INFINITY, 0.0f, {0.0f, 0.0f}};
-    const T *qp = static_cast<const T *>(q.data) + t * q.token_stride + h * q.head_stride;
-    row_forward(a, kv, load_row(qp, 0, a.dim), h, i + s.shift, 0, limit(a, s, i), st);
-    const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
-    const Row2 o{st.o.a * inv, st.o.b * inv};
-    store_row(static_cast<T *>(out.data) + t * out.token_stride + h * out.head_stride, o, a.dim);
-    if (out_low)
-        store_row(out_low + (t * a.heads + h) * a.dim,
-                  Row2{o.a - float(bf16(o.a)), o.b - float(bf16(o.b))}, a.dim);
-    if (lse && (threadIdx.x & 63) == 0)
-        lse[h * a.total_q + t] = st.l == 0.0f ? -INFINITY : (st.m + __log2f(st.l)) * kLn2;
+// Keys in splits: split n of a row has keys [n*chunk, (n+1)*chunk) of those it
+// sees, so a row that sees at most `chunk` keys has one split and is finished
+// by it. Others leave o (not yet divided), m and l in the workspace, and
+// k_attn_join adds them in order. chunk = 0: no splits.
+struct Split {
+    float *o;   // [splits][total_q*heads][dim]
+    float *ml;  // [splits][total_q*heads][2]
+    int32_t chunk;
+};
+
+template <class T>
+struct Output {
+    tc_rows out;
+    bf16 *low;
+    float *lse;
+};
+
+__device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
+__device__ __forceinline__ float log_sum(float m, float l) {
+    return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-tc_status forward(const char *fn, const tc_attn &p, const Source &src, int32_t cache_type,
-                  tc_rows q, tc_rows out, bf16 *out_low, float *lse, hipStream_t stream) {
-    const Args a = make_args(p);
-    const dim3 grid(p.max_q, p.num_heads, p.num_seqs);
-#define TC_LAUNCH(T, CT, PAGED)                                                                  \
-    hipLaunchKernelGGL((k_attn_rows<T, CT, PAGED>), grid, dim3(kWave), 0, stream, a, src, q, out, \
-                       out_low, lse)
-    if (p.dtype == TC_F32) {
+// What rounding left off, as a factor-free second store.
+template <class T>
+__device__ __forceinline__ void store_low(bf16 *row, const f32x16 &x, float f, int db, int dim) {
+    f32x16 y;
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+        const float v = x[r] * f;
+        y[r] = v - float(bf16(v));
+    }
+    store_block(row, y, 1.0f, db, dim);
+}
+
+// One query row computed by a wavefront: a row that sees a value that is not
+// finite in a tile that other rows of its block do not see in full.
+template <class T, class KV>
+__device__ void finish_row(const Args &a, const Seq &s, const KV &kv, tc_rows q,
+                           const Output<T> &o, const Split &sp, int h, int i, int j0, int split) {
+    const int64_t t = s.q0 + i, row = t * a.heads + h;
+    const int lim = limit(a, s, i);
+    if (split > 0 && j0 >= lim) return;
+    const bool whole = sp.chunk == 0 || lim <= sp.chunk;
+    RowState st{-INFINITY, 0.0f, {0.0f, 0.0f}};
+    const T *qp = static_cast<const T *>(q.data) + t * q.token_stride + h * q.head_stride;
+    row_forward(a, kv, load_row(qp, 0, a.dim), h, i + s.shift, j0,
+                whole ? lim : min(lim, j0 + sp.chunk), st);
+    const bool first = (threadIdx.x & 63) == 0;
+    if (whole) {
+        const float inv = inverse(st.l);
+        const Row2 x{st.o.a * inv, st.o.b * inv};
+        store_row(static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride, x,
+                  a.dim);
+        if (o.low)
+            store_row(o.low + row * a.dim, Row2{x.a - float(bf16(x.a)), x.b - float(bf16(x.b))},
+                      a.dim);
+        if (o.lse && first) o.lse[h * a.total_q + t] = log_sum(st.m, st.l);
+    } else {
+        const int64_t at = split * a.total_q * a.heads + row;
+        store_row(sp.o + at * a.dim, st.o, a.dim);
+        if (first) {
+            sp.ml[2 * at] = st.m;
+            sp.ml[2 * at + 1] = st.l;
+        }
+    }
+}
+
+// Attention of NW*32 queries of one head: a wavefront has 32 queries, the
+// workgroup shares tiles of BN keys and values in LDS.
+template <class T, class CT, bool PAGED, int DH, int NW, int BN>
+__global__ __launch_bounds__(NW * 64) void k_attn_tile(Args a, Source src, tc_rows q, Output<T> o,
+                                                       Split sp, int slots) {
+    typedef Tile<T, DH> Tl;
+    constexpr int BM = NW * 32, NT = NW * 64, CPR = DH / 8, IT = BN * CPR / NT;
+    static_assert(BN * CPR % NT == 0 && NT % CPR == 0, "");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int first_bad;  // first key whose value was cleaned
+    T *kt = reinterpret_cast<T *>(lds), *vt = kt + BN * DH;
+    float *bias = reinterpret_cast<float *>(vt + BN * DH);
+
+    // heads that share keys run on the same XCD (workgroups go round them);
+    // a sequence's last tiles, which see the most keys, come first
+    const int id = blockIdx.x;
+    const int kvh = id % a.kv_heads, h = kvh * a.group + (id / a.kv_heads) % a.group;
+    int tile;
+    const int b = seq_of_slot(a.q_off, a.num_seqs, slots - 1 - id / a.heads, BM, tile);
+    const Seq s = seq_at<PAGED>(a, src, b);
+    const int i0 = tile * BM;
+    if (i0 >= s.qn) return;
+    const int split = blockIdx.y, j0 = split * sp.chunk;
+    const int seen = limit(a, s, min(i0 + BM, s.qn) - 1);  // by the last query
+    const int end = sp.chunk ? min(seen, j0 + sp.chunk) : seen;
+    if (split > 0 && j0 >= seen) return;
+    const auto kv = KvOf<CT, PAGED>::make(src, s, kvh);
+
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, half = l >> 5;
+    const int w0 = i0 + wave * 32, i = w0 + (l & 31);
+    const int lim = limit(a, s, min(i, s.qn - 1));
+    const int lim_first = limit(a, s, min(w0, s.qn - 1)), lim_last = limit(a, s, min(w0 + 31, s.qn - 1));
+    const int block_first = limit(a, s, i0);
+    if (a.table) load_bias(a, h, bias);
+    if (threadIdx.x == 0) first_bad = INT32_MAX;
+
+    V8<T> qf[DH / 16];
+    {
+        const int64_t t = s.q0 + min(i, s.qn - 1);
+        const T *qp = static_cast<const T *>(q.data) + t * q.token_stride + h * q.head_stride;
+#pragma unroll
+        for (int ks = 0; ks < DH / 16; ks++) qf[ks] = chunk_of(qp, 2 * ks + half, a.dim);
+    }
+
+    f32x16 acc[DH / 32];
+#pragma unroll
+    for (int db = 0; db < DH / 32; db++) acc[db] = zero16();
+    float m = -INFINITY, sum = 0.0f;
+
+    const int row0 = threadIdx.x / CPR, col = threadIdx.x % CPR;
+    const bool live = col * 8 < a.dim;
+    Raw<CT> kr[IT], vr[IT];
+    auto fetch = [&](int kb) {
+#pragma unroll
+        for (int n = 0; n < IT; n++) {
+            const int j = kb + row0 + n * (NT / CPR);
+            kr[n] = zero_raw<CT>();
+            vr[n] = zero_raw<CT>();
+            if (j < end && live) {
+                const Loc at = kv.loc(j);
+                kr[n] = load_raw(kv.k(at) + col * 8, kv.k_exp(at));
+                vr[n] = load_raw(kv.v(at) + col * 8, kv.v_exp(at));
+            }
+        }
+    };
+    fetch(j0);
+    for (int kb = j0; kb < end; kb += BN) {
+        const bool mixed = min(kb + BN, end) > block_first;  // some rows see less of the tile
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < IT; n++) {
+            const int row = row0 + n * (NT / CPR);
+            V8<T> x;
+            expand(kr[n], x);
+            Tl::put(kt, row, col, x);
+            expand(vr[n], x);
+            if (mixed && clean(x)) atomicMin(&first_bad, kb + row);
+            Tl::put(vt, row, col, x);
+        }
+        __syncthreads();
+        if (kb + BN < end) fetch(kb + BN);
+        if (kb >= lim_last) continue;
+
+        f32x16 x[BN / 32];
+        float top = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < BN / 32; n++) {
+            const int k0 = kb + 32 * n;
+            x[n] = zero16();
+#pragma unroll
+            for (int ks = 0; ks < DH / 16; ks++) x[n] = mma(Tl::rows(kt, 32 * n, ks), qf[ks], x[n]);
+            if (a.capped) {
+#pragma unroll
+                for (int r = 0; r < 16; r++) x[n][r] = a.c2 * tanh_of(a.c1 * x[n][r]);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; r++) x[n][r] *= a.c1;
+            }
+            if (a.table) add_bias(a, bias, k0 - (w0 + s.shift), x[n]);
+            if (k0 + 32 > lim_first || k0 + 32 > end) {
+                const int left = min(lim, end) - k0 - 4 * half;
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    x[n][r] = reg_row(r) < left ? x[n][r] : -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; r++) top = fmaxf(top, x[n][r]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        // the subtracted value need not be the maximum, only near it: it moves
+        // when a score passes it by 2^8, which costs nothing in fp32 sums
+        if (__any(top > m + 8.0f)) {
+            const float next = fmaxf(m, top);
+            const float keep = next == -INFINITY ? 1.0f : exp2_fast(m - next);
+            m = next;
+            sum *= keep;
+#pragma unroll
+            for (int db = 0; db < DH / 32; db++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) acc[db][r] *= keep;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int n = 0; n < BN / 32; n++) {
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                x[n][r] = exp2_fast(x[n][r] - base);
+                sum += x[n][r];
+            }
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                V8<T> p;
+                pack(x[n], u, p);
+#pragma unroll
+                for (int db = 0; db < DH / 32; db++)
+                    acc[db] = mma(Tl::cols(vt, 32 * n + 16 * u, db), p, acc[db]);
+                if constexpr (sizeof(T) == 2) {
+                    if (o.low) {
+                        // the second half of the probabilities' bits: out and
+                        // out_low together then have 16 bits, which the bias
+                        // gradient's differences need
+                        pack_rest(x[n], u, p);
+#pragma unroll
+                        for (int db = 0; db < DH / 32; db++)
+                            acc[db] = mma(Tl::cols(vt, 32 * n + 16 * u, db), p, acc[db]);
+                    }
+                }
+            }
+        }
+    }
+
+    sum += __shfl_xor(sum, 32, kWave);
+    __syncthreads();
+    const int bad = first_bad;
+    if (bad < lim_last)
+        for (int r = 0; r < min(32, s.qn - w0); r++)
+            if (limit(a, s, w0 + r) > bad) finish_row(a, s, kv, q, o, sp, h, w0 + r, j0, split);
+    if (i >= s.qn || lim > bad) return;
+    const int64_t t = s.q0 + i, row = t * a.heads + h;
+    if (sp.chunk == 0 || lim <= sp.chunk) {
+        if (split > 0) return;
+        const float inv = inverse(sum);
+        T *op = static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride;
+#pragma unroll
+        for (int db = 0; db < DH / 32; db++) {
+            store_block(op, acc[db], inv, db, a.dim);
+            if (o.low) store_low<T>(o.low + row * a.dim, acc[db], inv, db, a.dim);
+        }
+        if (o.lse && half == 0) o.lse[h * a.total_q + t] = log_sum(m, sum);
+    } else if (j0 < lim) {
+        const int64_t at = split * a.total_q * a.heads + row;
+#pragma unroll
+        for (int db = 0; db < DH / 32; db++) store_block(sp.o + at * a.dim, acc[db], 1.0f, db, a.dim);
+        if (half == 0) {
+            sp.ml[2 * at] = m;
+            sp.ml[2 * at + 1] = sum;
+        }
+    }
+}
+
+// Attention of a few queries over many keys (decoding): the queries of all
+// heads that share a key head are the 32 columns of one block, row r being
+// query r / group, head r % group. Each wavefront takes every fourth block of
+// 32 keys for itself, so that nothing waits for another wavefront before the
+// end; keys go from memory to the operands directly (a lane reads row l%32),
+// values through a tile of the wavefront's own.
+template <class T, class CT, bool PAGED, int DH>
+__global__ __launch_bounds__(kBlock) void k_attn_few(Args a, Source src, tc_rows q, Output<T> o,
+                                                     Split sp, int row_tiles) {
+    typedef Tile<T, DH> Tl;
+    constexpr int KS = DH / 16, DB = DH / 32, NW = kBlock / 64;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float stat[NW][2][32];
+    __shared__ int first_bad;
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, half = l >> 5;
+    T *vt = reinterpret_cast<T *>(lds) + wave * 32 * DH;
+
+    int id = blockIdx.x;
+    const int kvh = id % a.kv_heads;
+    id /= a.kv_heads;
+    const int rt = id % row_tiles;
+    const Seq s = seq_at<PAGED>(a, src, id / row_tiles);
+    const int rows = min(s.qn * a.group - rt * 32, 32);  // of this workgroup
+    if (rows <= 0) return;
+    const int i_last = (rt * 32 + rows - 1) / a.group, i_first = rt * 32 / a.group;
+    const int split = blockIdx.y, j0 = split * sp.chunk;
+    const int seen = limit(a, s, i_last);
+    if (split > 0 && j0 >= seen) return;
+    const int end = sp.chunk ? min(seen, j0 + sp.chunk) : seen;
+    const int seen_first = limit(a, s, i_first);
+    const auto kv = KvOf<CT, PAGED>::make(src, s, kvh);
+    if (threadIdx.x == 0) first_bad = INT32_MAX;
+    __syncthreads();
+
+    const int r0 = rt * 32 + min(l & 31, rows - 1);
+    const int i = r0 / a.group, h = kvh * a.group + r0 % a.group;
+    const int64_t t = s.q0 + i;
+    const int lim = min(limit(a, s, i), end), pos = i + s.shift;
+    V8<T> qf[KS];
+    const T *qp = static_cast<const T *>(q.data) + t * q.token_stride + h * q.head_stride;
+#pragma unroll
+    for (int ks = 0; ks < KS; ks++) qf[ks] = chunk_of(qp, 2 * ks + half, a.dim);
+    const float far_left = a.table ? log2_bias(a, h, -a.reach) : 0.0f;
+    const float far_right = a.table ? log2_bias(a, h, a.reach) : 0.0f;
+
+    f32x16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; db++) acc[db] = zero16();
+    float m = -INFINITY, sum = 0.0f;
+
+    Raw<CT> kr[KS], vr[KS];
+    Loc next{};
+    auto locate = [&](int kb) {  // keys past the end repeat the last one
+        if (kb < end) next = kv.loc(min(kb + (l & 31), end - 1));
+    };
+    auto fetch_k = [&](const Loc &at) {
+        const uint32_t e = kv.k_exp(at);
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++)
+            kr[ks] = (2 * ks + half) * 8 < a.dim ? load_raw(kv.k(at) + (2 * ks + half) * 8, e)
+                                                 : zero_raw<CT>();
+    };
+    auto fetch_v = [&](const Loc &at, bool held) {
+        const uint32_t e = kv.v_exp(at);
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++)
+            vr[ks] = held && (2 * ks + half) * 8 < a.dim
+                         ? load_raw(kv.v(at) + (2 * ks + half) * 8, e)
+                         : zero_raw<CT>();
+    };
+    constexpr int STEP = 32 * NW;
+    int kb = j0 + wave * 32;
+    locate(kb);
+    if (kb < end) {
+        fetch_k(next);
+        fetch_v(next, kb + (l & 31) < end);
+    }
+    locate(kb + STEP);
+    for (; kb < end; kb += STEP) {
+        f32x16 x = zero16();
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) {
+            V8<T> k8;
+            expand(kr[ks], k8);
+            x = mma(k8, qf[ks], x);
+        }
+        const Loc at = next;
+        const bool more = kb + STEP < end;
+        if (more) fetch_k(at);
+        const bool mixed = min(kb + 32, end) > seen_first;
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) {
+            V8<T> v8;
+            expand(vr[ks], v8);
+            if (mixed && clean(v8)) atomicMin(&first_bad, kb + (l & 31));
+            Tl::put(vt, l & 31, 2 * ks + half, v8);
+        }
+        if (more) fetch_v(at, kb + STEP + (l & 31) < end);
+        locate(kb + 2 * STEP);
+
+        if (a.capped) {
+#pragma unroll
+            for (int r = 0; r < 16; r++) x[r] = a.c2 * tanh_of(a.c1 * x[r]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; r++) x[r] *= a.c1;
+        }
+        if (a.table) {
+            // distances of the block, over its queries
+            const int lo = kb - (i_last + s.shift), hi = kb + 31 - (i_first + s.shift);
+            if (hi <= -a.reach || lo >= a.reach) {
+                const float c = hi <= -a.reach ? far_left : far_right;
+#pragma unroll
+                for (int r = 0; r < 16; r++) x[r] += c;
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    x[r] += log2_bias(a, h, kb + 4 * half + reg_row(r) - pos);
+            }
+        }
+        if (kb + 32 > seen_first || kb + 32 > end) {
+            const int left = lim - kb - 4 * half;
+#pragma unroll
+            for (int r = 0; r < 16; r++) x[r] = reg_row(r) < left ? x[r] : -INFINITY;
+        }
+        float top = x[0];
+#pragma unroll
+        for (int r = 1; r < 16; r++) top = fmaxf(top, x[r]);
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        if (__any(top > m + 8.0f)) {
+            const float nm = fmaxf(m, top);
+            const float keep = nm == -INFINITY ? 1.0f : exp2_fast(m - nm);
+            m = nm;
+            sum *= keep;
+#pragma unroll
+            for (int db = 0; db < DB; db++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) acc[db][r] *= keep;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            x[r] = exp2_fast(x[r] - base);
+            sum += x[r];
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            V8<T> p;
+            pack(x, u, p);
+#pragma unroll
+            for (int db = 0; db < DB; db++) acc[db] = mma(Tl::cols(vt, 16 * u, db), p, acc[db]);
+            if constexpr (sizeof(T) == 2) {
+                if (o.low) {
+                    pack_rest(x, u, p);  // as in k_attn_tile
+#pragma unroll
+                    for (int db = 0; db < DB; db++)
+                        acc[db] = mma(Tl::cols(vt, 16 * u, db), p, acc[db]);
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    sum += __shfl_xor(sum, 32, kWave);
+
+    // the wavefronts' parts, added in order: half of the row at a time goes
+    // through LDS
+    if (half == 0) {
+        stat[wave][0][l] = m;
+        stat[wave][1][l] = sum;
+    }
+    __syncthreads();
+    const int bad = first_bad;
+    if (bad < seen)
+        for (int r = wave; r < rows; r += NW) {
+            const int gr = rt * 32 + r;
+            if (limit(a, s, gr / a.group) > bad)
+                finish_row(a, s, kv, q, o, sp, kvh * a.group + gr % a.group, gr / a.group, j0, split);
+        }
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; w++) top = fmaxf(top, stat[w][0][l & 31]);
+    const float mine = m == -INFINITY ? (sum == 0.0f ? 0.0f : sum) : exp2_fast(m - top);
+    constexpr int HD = DH / 2;  // elements at a time
+    float *buf = reinterpret_cast<float *>(lds);  // [NW][32][HD], 32*HD*4 = 32*DH*2 bytes each
+#pragma unroll
+    for (int p = 0; p < 2; p++) {
+        if (p) __syncthreads();
+        if ((l & 31) < rows) {
+#pragma unroll
+            for (int r4 = 0; r4 < HD / 8; r4++) {
+                const int e = p * (HD / 2) + 4 * r4;  // register of the half row
+                float y[4];
+#pragma unroll
+                for (int c = 0; c < 4; c++) y[c] = acc[(e + c) / 16][(e + c) % 16] * mine;
+                store4(buf + (wave * 32 + (l & 31)) * HD + 8 * r4 + 4 * half, y);
+            }
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < rows * (HD / 4); c += kBlock) {
+            const int r = c / (HD / 4), d = p * HD + (c % (HD / 4)) * 4;
+            if (d >= a.dim) continue;
+            f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+            float big = -INFINITY, total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; w++) big = fmaxf(big, stat[w][0][r]);
+#pragma unroll
+            for (int w = 0; w < NW; w++) {
+                const float mw = stat[w][0][r], lw = stat[w][1][r];
+                total += mw == -INFINITY ? lw : lw * exp2_fast(mw - big);
+                y += *reinterpret_cast<const f32x4 *>(buf + (w * 32 + r) * HD + (c % (HD / 4)) * 4);
+            }
+            const int gr = rt * 32 + r, qi = gr / a.group, qh = kvh * a.group + gr % a.group;
+            const int64_t tok = s.q0 + qi, row = tok * a.heads + qh;
+            const int full = limit(a, s, qi);
+            if (full > bad) continue;
+            if (sp.chunk == 0 || full <= sp.chunk) {
+                if (split > 0) continue;
+                const float inv = inverse(total);
+                const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+                store4(static_cast<T *>(o.out.data) + tok * o.out.token_stride +
+                           qh * o.out.head_stride + d, z);
+                if (o.low) {
+                    const float low[4] = {z[0] - float(bf16(z[0])), z[1] - float(bf16(z[1])),
+                                          z[2] - float(bf16(z[2])), z[3] - float(bf16(z[3]))};
+                    store4(o.low + row * a.dim + d, low);
+                }
+                if (o.lse && d == 0) o.lse[qh * a.total_q + tok] = log_sum(big, total);
+            } else if (j0 < full) {
+                const int64_t at = split * a.total_q * a.heads + row;
+                *reinterpret_cast<f32x4 *>(sp.o + at * a.dim + d) = y;
+                if (d == 0) {
+                    sp.ml[2 * at] = big;
+                    sp.ml[2 * at + 1] = total;
+                }
+            }
+        }
+    }
+}
+
+constexpr int kJoinWaves = 8;
+
+// Adds the splits of one row, where it has more than one: a workgroup per
+// (query, head), whose wavefronts take splits in turn.
+template <class T, bool PAGED>
+__global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(Args a, Source src, Output<T> o,
+                                                               Split sp) {
+    __shared__ float part[kJoinWaves][kMaxHeadDim + 2];
+    const int nw = blockDim.x >> 6, wave = threadIdx.x >> 6, l = threadIdx.x & 63;
+    const int64_t row = blockIdx.x, t = row / a.heads, rows = a.total_q * a.heads;
+    const int h = int(row - t * a.heads);
+    const int b = last_at_most(a.num_seqs, t, [&](int n) { return int64_t(a.q_off[n]); });
+    const Seq s = seq_at<PAGED>(a, src, b);
+    const int lim = limit(a, s, int(t - s.q0));
+    if (lim <= sp.chunk) return;
+    const int n = (lim + sp.chunk - 1) / sp.chunk;
+    float top = -INFINITY;
+    for (int k = l; k < n; k += kWave) top = fmaxf(top, sp.ml[2 * (k * rows + row)]);
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, kWave));
+    float x = 0.0f, y = 0.0f, total = 0.0f;
+#pragma unroll 4
+    for (int k = wave; k < n; k += nw) {
+        const int64_t at = k * rows + row;
+        const float m = sp.ml[2 * at], sum = sp.ml[2 * at + 1];
+        const float f = m == -INFINITY ? (sum == 0.0f ? 0.0f : sum) : exp2_fast(m - top);
+        total += m == -INFINITY ? sum : sum * f;
+        const float *p = sp.o + at * a.dim;
+        if (l < a.dim) x += p[l] * f;
+        if (l + 64 < a.dim) y += p[l + 64] * f;
+    }
+    part[wave][l] = x;
+    part[wave][l + 64] = y;
+    if (l == 0) part[wave][kMaxHeadDim] = total;
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < nw; w++) {
+        x += part[w][l];
+        y += part[w][l + 64];
+        total += part[w][kMaxHeadDim];
+    }
+    const float inv = inverse(total);
+    const Row2 r{x * inv, y * inv};
+    store_row(static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride, r,
+              a.dim);
+    if (o.low)
+        store_row(o.low + row * a.dim, Row2{r.a - float(bf16(r.a)), r.b - float(bf16(r.b))}, a.dim);
+    if (o.lse && l == 0) o.lse[h * a.total_q + t] = log_sum(top, total);
+}
+
+// --- launches ------------------------------------------------------------------
+
+// Which kernel and which splits a call takes, from its sizes alone.
+struct Plan {
+    bool few;
+    int waves;      // of a workgroup of k_attn_tile
+    int row_tiles;  // of k_attn_few
+    int64_t blocks;
+    int chunk, splits;
+};
+
+Plan plan_of(const tc_attn &a) {
+    Plan p{};
+    const int group = a.num_heads / a.num_kv_heads;
+    const int64_t rows = int64_t(a.max_q) * group;
+    p.few = rows <= 64 && a.max_k > 128;
+    p.row_tiles = int((rows + 31) / 32);
+    const int64_t mean = a.num_seqs ? a.total_q / a.num_seqs : 0;
+    p.waves = a.max_q <= 32 || mean <= 64 ? 1 : 4;
+    p.blocks = p.few ? int64_t(a.num_seqs) * a.num_kv_heads * p.row_tiles
+                     : tile_slots(a.total_q, a.num_seqs, 32 * p.waves) * a.num_heads;
+    p.splits = 1;
+    const int64_t want = int64_t(device_cus()) * (p.few ? 8 : 4);
+    if (p.blocks > 0 && p.blocks < want && a.max_k > 512) {
+        int64_t chunk = 256;
+        while (p.blocks * ((a.max_k + chunk - 1) / chunk) > want) chunk *= 2;
+        const int64_t n = (a.max_k + chunk - 1) / chunk;
+        if (n > 1) {
+            p.chunk = int(chunk);
+            p.splits = int(n);
+        }
+    }
+    return p;
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+size_t split_bytes(const tc_attn &a, const Plan &p, size_t *ml_at) {
+    if (p.splits <= 1) return 0;
+    const size_t rows = size_t(p.splits) * size_t(a.total_q) * size_t(a.num_heads);
+    *ml_at = up256(rows * size_t(a.head_dim) * sizeof(float));
+    return *ml_at + up256(rows * 2 * sizeof(float));
+}
+
+template <class T, class CT, bool PAGED, int DH>
+void launch(const tc_attn &t, const Args &a, const Plan &p, const Source &src, tc_rows q,
+            const Output<T> &o, const Split &sp, hipStream_t stream) {
+    constexpr int BN = sizeof(T) == 4 ? 32 : 64;
+    const dim3 grid(unsigned(p.blocks), p.splits);
+    if (p.few) {
+        hipLaunchKernelGGL((k_attn_few<T, CT, PAGED, DH>), grid, dim3(kBlock),
+                           4 * 32 * DH * sizeof(T), stream, a, src, q, o, sp, p.row_tiles);
+    } else {
+        const size_t bias = a.table ? bias_entries(a.reach) * sizeof(float) : 0;
+        const int slots = int(p.blocks / a.heads);
+        if (p.waves == 1)
+            hipLaunchKernelGGL((k_attn_tile<T, CT, PAGED, DH, 1, 32>), grid, dim3(64),
+                               2 * 32 * DH * sizeof(T) + bias, stream, a, src, q, o, sp, slots);
+        else
+            hipLaunchKernelGGL((k_attn_tile<T, CT, PAGED, DH, 4, BN>), grid, dim3(256),
+                               2 * BN * DH * sizeof(T) + bias, stream, a, src, q, o, sp, slots);
+    }
+    if (p.splits > 1) {
+        const int nw = p.splits >= 16 ? kJoinWaves : 1;
+        hipLaunchKernelGGL((k_attn_join<T, PAGED>), dim3(unsigned(t.total_q * t.num_heads)),
+                           dim3(nw * 64), 0, stream, a, src, o, sp);
+    }
+}
+
+tc_status forward(const char *fn, const tc_attn &t, const Source &src, int32_t cache_type,
+                  tc_rows q, tc_rows out, bf16 *out_low, float *lse, void *workspace,
+                  size_t workspace_bytes, hipStream_t stream) {
+    const Plan p = plan_of(t);
+    size_t ml_at = 0;
+    const size_t need = split_bytes(t, p, &ml_at);
+    TC_REQUIRE(need == 0 || (workspace && workspace_bytes >= need &&
+                             (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0),
+               TC_ERR_WORKSPACE, "%s: needs a 256-byte aligned workspace of %zu bytes, got %zu", fn,
+               need, workspace_bytes);
+    TC_REQUIRE(p.blocks < (int64_t(1) << 31) &&
+                   (p.splits == 1 || t.total_q * t.num_heads < (int64_t(1) << 31)),
+               TC_ERR_INVALID_ARG, "%s: more than 2^31 workgroups", fn);
+    const Args a = make_args(t);
+    Split sp{};
+    if (p.splits > 1) {
+        sp.o = static_cast<float *>(workspace);
+        sp.ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + ml_at);
+        sp.chunk = p.chunk;
+    }
+#define TC_LAUNCH(T, CT, PAGED)                                                           (t.head_dim <= 64                                                                          ? launch<T, CT, PAGED, 64>(t, a, p, src, q, {out, out_low, lse}, sp, stream)          : launch<T, CT, PAGED, 128>(t, a, p, src, q, {out, out_low, lse}, sp, stream))
+    if (t.dtype == TC_F32) {
         if (!src.paged)
             TC_LAUNCH(float, float, false);
         else if (cache_type == TC_FP8)
@@ -106,7 +705,14 @@ tc_status check_attn(const char *fn, const tc_attn *a, bool paged) {
 using namespace tc;
 using namespace tc::attn;
 
-extern "C" size_t tc_attn_workspace_bytes(const tc_attn *a, int32_t paged) { return 0; }
+extern "C" size_t tc_attn_workspace_bytes(const tc_attn *a, int32_t paged) {
+    (void)paged;
+    if (!a || a->num_seqs <= 0 || a->total_q <= 0 || a->max_q <= 0 || a->max_k <= 0 ||
+        a->num_kv_heads <= 0 || a->num_heads < a->num_kv_heads || a->head_dim <= 0)
+        return 0;
+    size_t ml_at = 0;
+    return split_bytes(*a, plan_of(*a), &ml_at);
+}
 
 extern "C" tc_status tc_attn_forward(const tc_attn *a, tc_rows q, tc_rows k, tc_rows v, tc_rows out,
                                      void *out_low, float *lse, void *workspace,
@@ -124,7 +730,7 @@ extern "C" tc_status tc_attn_forward(const tc_attn *a, tc_rows q, tc_rows k, tc_
                "%s: out_low is for TC_BF16 only", fn);
     TC_REQUIRE(aligned16(out_low), TC_ERR_UNSUPPORTED, "%s: out_low must be 16-byte aligned", fn);
     return forward(fn, *a, dense_source(k, v), a->dtype, q, out, static_cast<bf16 *>(out_low), lse,
-                   stream);
+                   workspace, workspace_bytes, stream);
 }
 
 extern "C" tc_status tc_attn_paged(const tc_attn *a, tc_rows q, const tc_cache *c, tc_rows out,
@@ -141,5 +747,6 @@ extern "C" tc_status tc_attn_paged(const tc_attn *a, tc_rows q, const tc_cache *
     TC_REQUIRE(c->page_table && c->lens, TC_ERR_INVALID_ARG, "%s: null pointer", fn);
     if ((st = check_rows(fn, "q", q, a->dtype, true)) != TC_OK) return st;
     if ((st = check_rows(fn, "out", out, a->dtype, true)) != TC_OK) return st;
-    return forward(fn, *a, paged_source(*c), c->dtype, q, out, nullptr, lse, stream);
+    return forward(fn, *a, paged_source(*c), c->dtype, q, out, nullptr, lse, workspace,
+                   workspace_bytes, stream);
 }
