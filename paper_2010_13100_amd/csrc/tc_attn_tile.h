@@ -303,5 +303,21 @@ __device__ __forceinline__ void add_bias(const Args &a, const float *lds, int re
     for (int r = 0; r < 16; r++) x[r] += p[reg_row(r)];
 }
 
+// The same for a block whose rows are queries: this lane's registers are
+// queries 4*half + reg_row(r), key col.
+__device__ __forceinline__ void add_bias_queries(const Args &a, const float *lds, int rel,
+                                                 f32x16 &x) {
+    const int l = threadIdx.x & 63;
+    if (rel + 31 <= -a.reach || rel - 31 >= a.reach) {
+        const float c = lds[rel < 0 ? 0 : 2 * (a.reach + kBiasPad)];
+#pragma unroll
+        for (int r = 0; r < 16; r++) x[r] += c;
+        return;
+    }
+    const float *p = lds + (rel - 4 * (l >> 5) + (l & 31) + a.reach + kBiasPad);
+#pragma unroll
+    for (int r = 0; r < 16; r++) x[r] += p[-reg_row(r)];
+}
+
 }  // namespace attn
 }  // namespace tc
