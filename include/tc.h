@@ -467,16 +467,13 @@ size_t tc_attn_backward_workspace_bytes(const tc_attn *a);
 /*
  * Attention forward: q [total_q x num_heads], k and v [total_k x
  * num_kv_heads], out [total_q x num_heads] written.
- *   out_low  NULL, or [total_q x num_heads x head_dim] bf16, contiguous,
- *            written: what rounding out to bf16 left off. Only for TC_BF16;
- *            tc_attn_backward takes it.
  *   lse      NULL, or [num_heads x total_q] floats, written: the natural
  *            log of the sum of exp(s) over the visible keys
  *   workspace device memory of tc_attn_workspace_bytes(a, 0) bytes,
  *            256-byte aligned; no initial contents are needed
  */
 tc_status tc_attn_forward(const tc_attn *a, tc_rows q, tc_rows k, tc_rows v, tc_rows out,
-                          void *out_low, float *lse, void *workspace, size_t workspace_bytes,
+                          float *lse, void *workspace, size_t workspace_bytes,
                           hipStream_t stream);
 
 /*
@@ -486,15 +483,14 @@ tc_status tc_attn_forward(const tc_attn *a, tc_rows q, tc_rows k, tc_rows v, tc_
  * share a key head), all written, and
  *   grad_bias  [num_buckets x num_heads] floats, written: the coalesced
  *              gradient of bias_table; NULL to leave it out, and NULL
- *              without a bias
- *   out_low    as written by the forward, or NULL: the row sums <grad_out,
- *              out> then carry out's rounding to bf16
+ *              without a bias. Where a NaN or an infinity is visible to a
+ *              query, entries may be NaN that the formula leaves finite.
  *   workspace  tc_attn_backward_workspace_bytes(a) bytes, 256-byte aligned
  */
 tc_status tc_attn_backward(const tc_attn *a, tc_rows q, tc_rows k, tc_rows v, tc_rows out,
-                           const void *out_low, const float *lse, tc_rows grad_out,
-                           tc_rows grad_q, tc_rows grad_k, tc_rows grad_v, float *grad_bias,
-                           void *workspace, size_t workspace_bytes, hipStream_t stream);
+                           const float *lse, tc_rows grad_out, tc_rows grad_q, tc_rows grad_k,
+                           tc_rows grad_v, float *grad_bias, void *workspace,
+                           size_t workspace_bytes, hipStream_t stream);
 
 /*
  * A paged cache of keys and values (host struct). Page p, slot s and key

@@ -20,7 +20,6 @@ struct Split {
 template <class T>
 struct Output {
     tc_rows out;
-    bf16 *low;
     float *lse;
 };
 
@@ -28,18 +27,6 @@ __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.
 
 __device__ __forceinline__ float log_sum(float m, float l) {
     return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-}
-
-// What rounding left off, as a factor-free second store.
-template <class T>
-__device__ __forceinline__ void store_low(bf16 *row, const f32x16 &x, float f, int db, int dim) {
-    f32x16 y;
-#pragma unroll
-    for (int r = 0; r < 16; r++) {
-        const float v = x[r] * f;
-        y[r] = v - float(bf16(v));
-    }
-    store_block(row, y, 1.0f, db, dim);
 }
 
 // One query row computed by a wavefront: a row that sees a value that is not
@@ -61,9 +48,6 @@ __device__ void finish_row(const Args &a, const Seq &s, const KV &kv, tc_rows q,
         const Row2 x{st.o.a * inv, st.o.b * inv};
         store_row(static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride, x,
                   a.dim);
-        if (o.low)
-            store_row(o.low + row * a.dim, Row2{x.a - float(bf16(x.a)), x.b - float(bf16(x.b))},
-                      a.dim);
         if (o.lse && first) o.lse[h * a.total_q + t] = log_sum(st.m, st.l);
     } else {
         const int64_t at = split * a.total_q * a.heads + row;
@@ -78,10 +62,11 @@ __device__ void finish_row(const Args &a, const Seq &s, const KV &kv, tc_rows q,
 // Attention of NW*32 queries of one head: a wavefront has 32 queries, the
 // workgroup shares tiles of BN keys and values in LDS.
 template <class T, class CT, bool PAGED, int DH, int NW, int BN>
-__global__ __launch_bounds__(NW * 64) void k_attn_tile(Args a, Source src, tc_rows q, Output<T> o,
+__global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_tile(Args a, Source src, tc_rows q, Output<T> o,
                                                        Split sp, int slots) {
     typedef Tile<T, DH> Tl;
     constexpr int BM = NW * 32, NT = NW * 64, CPR = DH / 8, IT = BN * CPR / NT;
+    constexpr bool AHEAD = NW > 1;  // a lone wavefront has no registers for it
     static_assert(BN * CPR % NT == 0 && NT % CPR == 0, "");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int first_bad;  // first key whose value was cleaned
@@ -140,9 +125,10 @@ __global__ __launch_bounds__(NW * 64) void k_attn_tile(Args a, Source src, tc_ro
             }
         }
     };
-    fetch(j0);
+    if (AHEAD) fetch(j0);
     for (int kb = j0; kb < end; kb += BN) {
         const bool mixed = min(kb + BN, end) > block_first;  // some rows see less of the tile
+        if (!AHEAD) fetch(kb);
         __syncthreads();
 #pragma unroll
         for (int n = 0; n < IT; n++) {
@@ -155,7 +141,7 @@ __global__ __launch_bounds__(NW * 64) void k_attn_tile(Args a, Source src, tc_ro
             Tl::put(vt, row, col, x);
         }
         __syncthreads();
-        if (kb + BN < end) fetch(kb + BN);
+        if (AHEAD && kb + BN < end) fetch(kb + BN);
         if (kb >= lim_last) continue;
 
         f32x16 x[BN / 32];
@@ -211,17 +197,6 @@ __global__ __launch_bounds__(NW * 64) void k_attn_tile(Args a, Source src, tc_ro
 #pragma unroll
                 for (int db = 0; db < DH / 32; db++)
                     acc[db] = mma(Tl::cols(vt, 32 * n + 16 * u, db), p, acc[db]);
-                if constexpr (sizeof(T) == 2) {
-                    if (o.low) {
-                        // the second half of the probabilities' bits: out and
-                        // out_low together then have 16 bits, which the bias
-                        // gradient's differences need
-                        pack_rest(x[n], u, p);
-#pragma unroll
-                        for (int db = 0; db < DH / 32; db++)
-                            acc[db] = mma(Tl::cols(vt, 32 * n + 16 * u, db), p, acc[db]);
-                    }
-                }
             }
         }
     }
@@ -239,10 +214,7 @@ __global__ __launch_bounds__(NW * 64) void k_attn_tile(Args a, Source src, tc_ro
         const float inv = inverse(sum);
         T *op = static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride;
 #pragma unroll
-        for (int db = 0; db < DH / 32; db++) {
-            store_block(op, acc[db], inv, db, a.dim);
-            if (o.low) store_low<T>(o.low + row * a.dim, acc[db], inv, db, a.dim);
-        }
+        for (int db = 0; db < DH / 32; db++) store_block(op, acc[db], inv, db, a.dim);
         if (o.lse && half == 0) o.lse[h * a.total_q + t] = log_sum(m, sum);
     } else if (j0 < lim) {
         const int64_t at = split * a.total_q * a.heads + row;
@@ -262,7 +234,7 @@ __global__ __launch_bounds__(NW * 64) void k_attn_tile(Args a, Source src, tc_ro
 // end; keys go from memory to the operands directly (a lane reads row l%32),
 // values through a tile of the wavefront's own.
 template <class T, class CT, bool PAGED, int DH>
-__global__ __launch_bounds__(kBlock) void k_attn_few(Args a, Source src, tc_rows q, Output<T> o,
+__global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_few(Args a, Source src, tc_rows q, Output<T> o,
                                                      Split sp, int row_tiles) {
     typedef Tile<T, DH> Tl;
     constexpr int KS = DH / 16, DB = DH / 32, NW = kBlock / 64;
@@ -407,14 +379,6 @@ __global__ __launch_bounds__(kBlock) void k_attn_few(Args a, Source src, tc_rows
             pack(x, u, p);
 #pragma unroll
             for (int db = 0; db < DB; db++) acc[db] = mma(Tl::cols(vt, 16 * u, db), p, acc[db]);
-            if constexpr (sizeof(T) == 2) {
-                if (o.low) {
-                    pack_rest(x, u, p);  // as in k_attn_tile
-#pragma unroll
-                    for (int db = 0; db < DB; db++)
-                        acc[db] = mma(Tl::cols(vt, 16 * u, db), p, acc[db]);
-                }
-            }
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -477,11 +441,6 @@ __global__ __launch_bounds__(kBlock) void k_attn_few(Args a, Source src, tc_rows
                 const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
                 store4(static_cast<T *>(o.out.data) + tok * o.out.token_stride +
                            qh * o.out.head_stride + d, z);
-                if (o.low) {
-                    const float low[4] = {z[0] - float(bf16(z[0])), z[1] - float(bf16(z[1])),
-                                          z[2] - float(bf16(z[2])), z[3] - float(bf16(z[3]))};
-                    store4(o.low + row * a.dim + d, low);
-                }
                 if (o.lse && d == 0) o.lse[qh * a.total_q + tok] = log_sum(big, total);
             } else if (j0 < full) {
                 const int64_t at = split * a.total_q * a.heads + row;
@@ -540,8 +499,6 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(Args a, Source sr
     const Row2 r{x * inv, y * inv};
     store_row(static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride, r,
               a.dim);
-    if (o.low)
-        store_row(o.low + row * a.dim, Row2{r.a - float(bf16(r.a)), r.b - float(bf16(r.b))}, a.dim);
     if (o.lse && l == 0) o.lse[h * a.total_q + t] = log_sum(top, total);
 }
 
@@ -615,7 +572,7 @@ void launch(const tc_attn &t, const Args &a, const Plan &p, const Source &src, t
 }
 
 tc_status forward(const char *fn, const tc_attn &t, const Source &src, int32_t cache_type,
-                  tc_rows q, tc_rows out, bf16 *out_low, float *lse, void *workspace,
+                  tc_rows q, tc_rows out, float *lse, void *workspace,
                   size_t workspace_bytes, hipStream_t stream) {
     const Plan p = plan_of(t);
     size_t ml_at = 0;
@@ -634,7 +591,7 @@ tc_status forward(const char *fn, const tc_attn &t, const Source &src, int32_t c
         sp.ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + ml_at);
         sp.chunk = p.chunk;
     }
-#define TC_LAUNCH(T, CT, PAGED)                                                           (t.head_dim <= 64                                                                          ? launch<T, CT, PAGED, 64>(t, a, p, src, q, {out, out_low, lse}, sp, stream)          : launch<T, CT, PAGED, 128>(t, a, p, src, q, {out, out_low, lse}, sp, stream))
+#define TC_LAUNCH(T, CT, PAGED)                                                           (t.head_dim <= 64                                                                          ? launch<T, CT, PAGED, 64>(t, a, p, src, q, {out, lse}, sp, stream)          : launch<T, CT, PAGED, 128>(t, a, p, src, q, {out, lse}, sp, stream))
     if (t.dtype == TC_F32) {
         if (!src.paged)
             TC_LAUNCH(float, float, false);
@@ -715,8 +672,7 @@ extern "C" size_t tc_attn_workspace_bytes(const tc_attn *a, int32_t paged) {
 }
 
 extern "C" tc_status tc_attn_forward(const tc_attn *a, tc_rows q, tc_rows k, tc_rows v, tc_rows out,
-                                     void *out_low, float *lse, void *workspace,
-                                     size_t workspace_bytes, hipStream_t stream) {
+                                     float *lse, void *workspace, size_t workspace_bytes, hipStream_t stream) {
     const char *fn = "tc_attn_forward";
     clear_error();
     tc_status st = check_attn(fn, a, false);
@@ -726,11 +682,8 @@ extern "C" tc_status tc_attn_forward(const tc_attn *a, tc_rows q, tc_rows k, tc_
     if ((st = check_rows(fn, "k", k, a->dtype, a->total_k > 0)) != TC_OK) return st;
     if ((st = check_rows(fn, "v", v, a->dtype, a->total_k > 0)) != TC_OK) return st;
     if ((st = check_rows(fn, "out", out, a->dtype, true)) != TC_OK) return st;
-    TC_REQUIRE(!out_low || a->dtype == TC_BF16, TC_ERR_INVALID_ARG,
-               "%s: out_low is for TC_BF16 only", fn);
-    TC_REQUIRE(aligned16(out_low), TC_ERR_UNSUPPORTED, "%s: out_low must be 16-byte aligned", fn);
-    return forward(fn, *a, dense_source(k, v), a->dtype, q, out, static_cast<bf16 *>(out_low), lse,
-                   workspace, workspace_bytes, stream);
+    return forward(fn, *a, dense_source(k, v), a->dtype, q, out, lse, workspace,
+                   workspace_bytes, stream);
 }
 
 extern "C" tc_status tc_attn_paged(const tc_attn *a, tc_rows q, const tc_cache *c, tc_rows out,
@@ -747,6 +700,6 @@ extern "C" tc_status tc_attn_paged(const tc_attn *a, tc_rows q, const tc_cache *
     TC_REQUIRE(c->page_table && c->lens, TC_ERR_INVALID_ARG, "%s: null pointer", fn);
     if ((st = check_rows(fn, "q", q, a->dtype, true)) != TC_OK) return st;
     if ((st = check_rows(fn, "out", out, a->dtype, true)) != TC_OK) return st;
-    return forward(fn, *a, paged_source(*c), c->dtype, q, out, nullptr, lse, workspace,
+    return forward(fn, *a, paged_source(*c), c->dtype, q, out, lse, workspace,
                    workspace_bytes, stream);
 }

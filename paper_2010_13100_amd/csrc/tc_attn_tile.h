@@ -62,14 +62,6 @@ __device__ __forceinline__ void pack(const f32x16 &x, int s, f32x8 &f) {
     for (int i = 0; i < 8; i++) f[i] = x[8 * s + i];
 }
 
-// The same of what rounding to bf16 leaves off (fp32: nothing).
-__device__ __forceinline__ void pack_rest(const f32x16 &x, int s, bf16x8 &f) {
-    f32x16 y;
-#pragma unroll
-    for (int i = 8 * s; i < 8 * s + 8; i++) y[i] = x[i] - float(bf16(x[i]));
-    pack(y, s, f);
-}
-
 // --- 8 elements from memory ---------------------------------------------------
 
 template <class CT>

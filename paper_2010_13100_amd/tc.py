@@ -75,9 +75,9 @@ _SIGNATURES = {
     "tc_check_index": (_i32, [_vp, _i32, _i32, _i64, _i64, _vp, _vp, _i64, _vp, _vp]),
     "tc_attn_workspace_bytes": (_sz, [_attn_p, _i32]),
     "tc_attn_backward_workspace_bytes": (_sz, [_attn_p]),
-    "tc_attn_forward": (_i32, [_attn_p, TcRows, TcRows, TcRows, TcRows, _vp, _vp, _vp, _sz, _vp]),
-    "tc_attn_backward": (_i32, [_attn_p, TcRows, TcRows, TcRows, TcRows, _vp, _vp, TcRows, TcRows,
-                                TcRows, TcRows, _vp, _vp, _sz, _vp]),
+    "tc_attn_forward": (_i32, [_attn_p, TcRows, TcRows, TcRows, TcRows, _vp, _vp, _sz, _vp]),
+    "tc_attn_backward": (_i32, [_attn_p, TcRows, TcRows, TcRows, TcRows, _vp, TcRows, TcRows, TcRows,
+                                TcRows, _vp, _vp, _sz, _vp]),
     "tc_attn_paged": (_i32, [_attn_p, TcRows, _cache_p, TcRows, _vp, _vp, _sz, _vp]),
     "tc_cache_write": (_i32, [_cache_p, _i32, _i32, _vp, _i64, TcRows, TcRows, _vp]),
     "tc_cache_read": (_i32, [_cache_p, _i32, _i32, _vp, _i64, TcRows, TcRows, _vp]),
@@ -312,20 +312,18 @@ def tc_attn_backward_workspace_bytes(attn: TcAttn) -> int:
     return int(_lib.tc_attn_backward_workspace_bytes(attn))
 
 
-def tc_attn_forward(attn: TcAttn, q, k, v, out, out_low=None, lse=None, workspace=None,
-                    stream=None) -> None:
+def tc_attn_forward(attn: TcAttn, q, k, v, out, lse=None, workspace=None, stream=None) -> None:
     dt, h, kv, d = _attn_layout(attn)
     _same_tokens("tc_attn_forward", attn.total_q, ("q", q), ("out", out))
     _same_tokens("tc_attn_forward", attn.total_k, ("k", k), ("v", v))
     _check(_lib.tc_attn_forward(
         attn, _rows(q, dt, "q", h, d), _rows(k, dt, "k", kv, d), _rows(v, dt, "v", kv, d),
-        _rows(out, dt, "out", h, d), _sized(out_low, torch.bfloat16, "out_low",
-                                            attn.total_q * h * d),
+        _rows(out, dt, "out", h, d),
         _sized(lse, torch.float32, "lse", h * attn.total_q), *_ws(workspace), _stream(stream)),
         "tc_attn_forward")
 
 
-def tc_attn_backward(attn: TcAttn, q, k, v, out, out_low, lse, grad_out, grad_q, grad_k, grad_v,
+def tc_attn_backward(attn: TcAttn, q, k, v, out, lse, grad_out, grad_q, grad_k, grad_v,
                      grad_bias=None, workspace=None, stream=None) -> None:
     dt, h, kv, d = _attn_layout(attn)
     _same_tokens("tc_attn_backward", attn.total_q, ("q", q), ("out", out),
@@ -334,8 +332,7 @@ def tc_attn_backward(attn: TcAttn, q, k, v, out, out_low, lse, grad_out, grad_q,
                  ("grad_v", grad_v))
     _check(_lib.tc_attn_backward(
         attn, _rows(q, dt, "q", h, d), _rows(k, dt, "k", kv, d), _rows(v, dt, "v", kv, d),
-        _rows(out, dt, "out", h, d), _sized(out_low, torch.bfloat16, "out_low",
-                                            attn.total_q * h * d),
+        _rows(out, dt, "out", h, d),
         _sized(lse, torch.float32, "lse", h * attn.total_q),
         _rows(grad_out, dt, "grad_out", h, d), _rows(grad_q, dt, "grad_q", h, d),
         _rows(grad_k, dt, "grad_k", kv, d), _rows(grad_v, dt, "grad_v", kv, d),
@@ -510,11 +507,9 @@ class BagAttention:
         new = dict(dtype=dtype, device=device)
         self.out = torch.empty((total_q, num_heads, head_dim), **new)
         ws = tc_attn_workspace_bytes(self.attn, paged)
-        self.lse = self.out_low = self.grad_bias = None
+        self.lse = self.grad_bias = None
         if train:
             self.lse = torch.empty((num_heads, total_q), dtype=torch.float32, device=device)
-            if dtype == torch.bfloat16:
-                self.out_low = torch.empty_like(self.out)
             self.dq = torch.empty_like(self.out)
             self.dk = torch.empty((total_k, kv, head_dim), **new)
             self.dv = torch.empty_like(self.dk)
@@ -534,7 +529,7 @@ class BagAttention:
         """Attention of q over k, v ([tokens, heads, dim]; k_offsets defaults
         to q_offsets) into self.out."""
         a = self._bind(q_offsets, q_offsets if k_offsets is None else k_offsets, prefix_lens)
-        tc_attn_forward(a, q, k, v, self.out, self.out_low, self.lse, self.workspace, stream)
+        tc_attn_forward(a, q, k, v, self.out, self.lse, self.workspace, stream)
         return self.out
 
     def backward(self, q, k, v, grad_out, q_offsets, k_offsets=None, prefix_lens=None,
@@ -544,7 +539,7 @@ class BagAttention:
         if self.lse is None:
             raise ValueError("BagAttention.backward needs train=True")
         a = self._bind(q_offsets, q_offsets if k_offsets is None else k_offsets, prefix_lens)
-        tc_attn_backward(a, q, k, v, self.out, self.out_low, self.lse, grad_out, self.dq, self.dk,
+        tc_attn_backward(a, q, k, v, self.out, self.lse, grad_out, self.dq, self.dk,
                          self.dv, self.grad_bias, self.workspace, stream)
 
     def forward_paged(self, q, cache: PagedCache, q_offsets, page_table, lens, prefix_lens=None,

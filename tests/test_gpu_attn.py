@@ -79,7 +79,7 @@ def make(q_lens, k_lens=None, *, heads=1, kv=None, dim=64, dtype=F32, causal=Fal
 
 
 def poison(a):
-    for n in ("out", "lse", "out_low", "dq", "dk", "dv", "grad_bias", "workspace"):
+    for n in ("out", "lse", "dq", "dk", "dv", "grad_bias", "workspace"):
         t = getattr(a, n, None)
         if t is not None:
             t.view(torch.uint8).fill_(0xff)  # NaN in every type
