@@ -420,8 +420,9 @@ tc_status tc_check_index(const int64_t *table_row_offset, int32_t num_tables,
  * Layout: rows are found by strides in elements (tc_rows), so one array
  * may hold q, k and v side by side, or heads may be outermost. The head_dim
  * elements of a row are contiguous, head_dim is a multiple of 8 in [8, 128],
- * every row starts at a multiple of 16 bytes (TC_ERR_UNSUPPORTED otherwise;
- * 8-bit caches: of 8 bytes). Arrays may be larger than 2^31 elements.
+ * every row starts at a multiple of 16 bytes (8-bit caches: of 8 bytes) and
+ * token strides are below 2^24 (TC_ERR_UNSUPPORTED otherwise). Arrays may be
+ * larger than 2^31 elements.
  */
 typedef enum tc_dtype {
     TC_F32 = 0,

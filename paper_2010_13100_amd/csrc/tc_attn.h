@@ -110,9 +110,15 @@ __device__ __forceinline__ int first_query(const Args &a, const Seq &s, int j) {
     return min(max(j - s.shift, 0), s.qn);
 }
 
-// tanh of the scaled product, from c1*z.
-__device__ __forceinline__ float tanh_of(float y) {
-    return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + exp2_fast(y)), 1.0f);
+// 1/(1 + exp2(y)), y = c1*z: tanh is 1 - 2r, its derivative 4*(r - r*r).
+__device__ __forceinline__ float half_tanh(float y) {
+    return __builtin_amdgcn_rcpf(1.0f + exp2_fast(y));
+}
+
+// The score of product z, plus c0.
+__device__ __forceinline__ float score(const Args &a, float z, float c0) {
+    if (!a.capped) return __builtin_fmaf(z, a.c1, c0);
+    return __builtin_fmaf(-2.0f * a.c2, half_tanh(a.c1 * z), a.c2 + c0);
 }
 
 __device__ __forceinline__ float log2_bias(const Args &a, int h, int delta) {
@@ -158,10 +164,26 @@ struct Loc {
     int64_t e;     // of the exponent bytes
 };
 
+// n / d for n < 2^31 and d in [1, 2^20] as a product: m = floor(2^(31+s)/d) + 1
+// with s = ceil(log2 d) exceeds 2^(31+s)/d by at most 2^s/d, which is too
+// little to reach the next quotient.
+struct Divider {
+    uint32_t d, m, s;
+};
+inline Divider make_divider(uint32_t d) {
+    uint32_t s = 0;
+    while ((uint32_t(1) << s) < d) s++;
+    return {d, uint32_t((uint64_t(1) << (31 + s)) / d + 1), s};
+}
+__device__ __forceinline__ int divide(int n, const Divider &v) {
+    return int(__umulhi(v.m, uint32_t(n) * 2u) >> v.s);
+}
+
 // Keys of one sequence and key head in [token][head] rows.
 template <class CT>
 struct DenseKv {
     typedef CT type;
+    static constexpr bool paged = false;
     const CT *kp, *vp;
     int64_t kts, vts;
     __device__ __forceinline__ Loc loc(int j) const { return {j * kts, j * vts, 0}; }
@@ -175,29 +197,37 @@ struct DenseKv {
 template <class CT>
 struct PagedKv {
     typedef CT type;
-    const CT *kp, *vp;        // with the head's offset
-    const uint8_t *ke, *ve;   // with the head's offset
-    const int32_t *pages;     // of the sequence
+    static constexpr bool paged = true;
+    const CT *kp, *vp;       // with the head's offset
+    const uint8_t *ke, *ve;  // with the head's offset
+    const int32_t *pages;    // of the sequence
     int64_t page_stride, slot_stride;
-    int32_t page_size, shift, kv_heads;  // shift: log2 page_size, or -1
-    __device__ __forceinline__ Loc loc(int j) const {
-        const int p = shift >= 0 ? j >> shift : int(uint32_t(j) / uint32_t(page_size));
-        const int s = j - p * page_size;
-        const int64_t page = pages[p];
+    Divider page_size;
+    int32_t kv_heads;
+    // the page of key j, to be looked up before its rows are needed
+    __device__ __forceinline__ int page(int j) const { return pages[divide(j, page_size)]; }
+    __device__ __forceinline__ Loc loc(int j, int page) const {
+        const int s = j - divide(j, page_size) * int(page_size.d);
         const int64_t o = page * page_stride + s * slot_stride;
-        return {o, o, (page * page_size + s) * kv_heads};
+        return {o, o, (int64_t(page) * page_size.d + s) * kv_heads};
     }
+    __device__ __forceinline__ Loc loc(int j) const { return loc(j, page(j)); }
     __device__ __forceinline__ const CT *k(const Loc &l) const { return kp + l.k; }
     __device__ __forceinline__ const CT *v(const Loc &l) const { return vp + l.v; }
-    __device__ __forceinline__ uint32_t k_exp(const Loc &l) const { return ke ? ke[l.e] : 127; }
-    __device__ __forceinline__ uint32_t v_exp(const Loc &l) const { return ve ? ve[l.e] : 127; }
+    __device__ __forceinline__ uint32_t k_exp(const Loc &l) const {
+        return sizeof(CT) == 1 ? ke[l.e] : 127;
+    }
+    __device__ __forceinline__ uint32_t v_exp(const Loc &l) const {
+        return sizeof(CT) == 1 ? ve[l.e] : 127;
+    }
 };
 
 // Where a call's keys come from: dense rows, or a cache.
 struct Source {
     tc_rows k, v;    // dense
     tc_cache cache;  // paged
-    int32_t paged, page_shift;
+    Divider page_size;
+    int32_t paged;
 };
 
 inline Source dense_source(tc_rows k, tc_rows v) {
@@ -211,9 +241,7 @@ inline Source paged_source(const tc_cache &c) {
     Source s{};
     s.cache = c;
     s.paged = 1;
-    s.page_shift = -1;
-    for (int b = 0; b < 31; b++)
-        if ((1 << b) == c.page_size) s.page_shift = b;
+    s.page_size = make_divider(uint32_t(c.page_size));
     return s;
 }
 
@@ -247,8 +275,7 @@ struct KvOf<CT, true> {
                 c.page_table + int64_t(q.b) * c.max_pages,
                 c.page_stride,
                 c.slot_stride,
-                c.page_size,
-                s.page_shift,
+                s.page_size,
                 c.num_kv_heads};
     }
 };
@@ -300,8 +327,7 @@ __device__ void row_forward(const Args &a, const KV &kv, Row2 q, int h, int pos,
     for (int j = j0; j < j1; j++) {
         const Loc l = kv.loc(j);
         const float z = dot(q, load_row(kv.k(l), kv.k_exp(l), a.dim));
-        float s = a.capped ? a.c2 * tanh_of(a.c1 * z) : a.c1 * z;
-        if (a.table) s += log2_bias(a, h, j - pos);
+        const float s = score(a, z, a.table ? log2_bias(a, h, j - pos) : 0.0f);
         const float m = fmaxf(st.m, s), base = m == -INFINITY ? 0.0f : m;
         const float keep = exp2_fast(st.m - base), p = exp2_fast(s - base);
         const Row2 v = load_row(kv.v(l), kv.v_exp(l), a.dim);

@@ -16,18 +16,17 @@ struct Grads {
     int64_t total_k;
 };
 
-// One pair (query, key): p, and ds = p * (dp - delta) with respect to s.
+// One pair (query, key): p, ds = p * (dp - delta) with respect to s, and g with
+// respect to the product.
 __device__ __forceinline__ void pair_grad(const Args &a, float z, float bias, float lse2, float dp,
                                           float delta, float &p, float &ds, float &g) {
-    float t = 0.0f, x = a.c1 * z;
-    if (a.capped) {
-        t = tanh_of(x);
-        x = a.c2 * t;
-    }
-    p = exp2_fast(x + bias - lse2);
+    p = exp2_fast(score(a, z, bias) - lse2);
     ds = p * (dp - delta);
     g = ds * a.scale;
-    if (a.capped) g *= 1.0f - t * t;
+    if (a.capped) {
+        const float t = half_tanh(a.c1 * z);
+        g *= 4.0f * __builtin_fmaf(-t, t, t);
+    }
 }
 
 template <class T>
@@ -96,10 +95,10 @@ __device__ void row_dkv(const Args &a, const Grads &g, const Seq &s, int j, int 
 
 // Adds the entries of a block of ds (rows are queries, columns keys, distance
 // `rel` at row 0, column 0) to the sums by distance, which belong to this
-// wavefront. Entry (query, key) goes to row (key - query) mod 32 of `buf`, whose
-// 32 entries are those of two distances, r for the keys from r on and r - 32 for
-// those before; a lane adds up half a row.
-constexpr int kSkew = 33;
+// wavefront. 16 queries at a time, entry (query, key) goes to row (key - query)
+// mod 32 of `buf`, whose 16 entries are those of two distances, r and, where the
+// key would pass 32, r - 32; a lane adds up half a row.
+constexpr int kSkew = 17, kSkewFloats = 32 * kSkew;
 __device__ __forceinline__ void add_distances(const Args &a, const f32x16 &ds, int rel, float *buf,
                                               float *dist, float &far_left, float &far_right) {
     const int l = threadIdx.x & 63, half = l >> 5, c = l & 31;
@@ -113,18 +112,25 @@ __device__ __forceinline__ void add_distances(const Args &a, const f32x16 &ds, i
             far_right += x;
         return;
     }
-#pragma unroll
-    for (int r = 0; r < 16; r++) buf[((c - 4 * half - reg_row(r)) & 31) * kSkew + c] = ds[r];
-    __builtin_amdgcn_wave_barrier();
     float lo = 0.0f, hi = 0.0f;  // of distance c, of distance c - 32
 #pragma unroll
-    for (int n = 0; n < 16; n++) {
-        const int col = 16 * half + n;
-        const float x = buf[c * kSkew + col];
-        lo += col >= c ? x : 0.0f;
-        hi += col >= c ? 0.0f : x;
+    for (int p = 0; p < 2; p++) {
+#pragma unroll
+        for (int r = 8 * p; r < 8 * p + 8; r++) {
+            const int q = 4 * half + reg_row(r);
+            buf[((c - q) & 31) * kSkew + q - 16 * p] = ds[r];
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int n = 0; n < 8; n++) {
+            const int q = 8 * half + n;
+            const float x = buf[c * kSkew + q];
+            const bool first = c + q + 16 * p < 32;
+            lo += first ? x : 0.0f;
+            hi += first ? 0.0f : x;
+        }
+        __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
     lo += __shfl_xor(lo, 32, kWave);
     hi += __shfl_xor(hi, 32, kWave);
     const int d = rel + (half ? c - 32 : c);
@@ -138,22 +144,24 @@ __device__ __forceinline__ void add_distances(const Args &a, const f32x16 &ds, i
 }
 
 // Gradient of the queries. A wavefront has 32 queries, the workgroup shares
-// tiles of BN keys and values.
+// tiles of BN keys and values. With NBUF = 2 the next tile arrives while one is
+// worked on; a lone wavefront, whose share of a tile is four times as large, has
+// no registers for that.
 //
 // delta = sum_j p_j dp_j is <grad_out, out>, but out has been rounded, and the
 // bias gradient adds up so many terms p*(dp - delta) that cancel that this
 // shows. The terms of a row add up to 0, so what they do add up to here is
 // the error of delta: k_attn_dkv gets the sum of the two, exact to fp32.
-template <class T, int DH, int NW, int BN>
-__global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_dq(Args a, Grads g, int slots) {
+template <class T, bool CAP, int DH, int NW, int BN, int NBUF>
+__global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_dq(Args a, Grads g,
+                                                                                    int slots) {
     typedef Tile<T, DH> Tl;
-    constexpr int BM = NW * 32, NT = NW * 64, CPR = DH / 8, IT = BN * CPR / NT;
-    constexpr int KS = DH / 16, DB = DH / 32;
-    constexpr bool AHEAD = NW > 1;  // a lone wavefront has no registers for it
+    const typename Tl::Lane ln = Tl::lane();
+    constexpr int BM = NW * 32, NT = NW * 64, KS = DH / 16, DB = DH / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int first_bad;
-    T *kt = reinterpret_cast<T *>(lds), *vt = kt + BN * DH;
-    float *bias = reinterpret_cast<float *>(vt + BN * DH);
+    T *tiles = reinterpret_cast<T *>(lds);  // [NBUF][keys, values][BN][DH]
+    float *bias = reinterpret_cast<float *>(tiles + NBUF * 2 * BN * DH);
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, half = l >> 5;
     const int id = blockIdx.x;
     const int kvh = id % a.kv_heads, h = kvh * a.group + (id / a.kv_heads) % a.group;
@@ -163,15 +171,17 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
     const int i0 = tile * BM;
     if (i0 >= s.qn) return;
     const int end = limit(a, s, min(i0 + BM, s.qn) - 1), block_first = limit(a, s, i0);
-    const auto kv = KvOf<T, false>::make({g.k, g.v, {}, 0, 0}, s, kvh);
+    const auto kv = KvOf<T, false>::make({g.k, g.v, {}, {}, 0}, s, kvh);
     const int w0 = i0 + wave * 32, i = w0 + (l & 31);
     const int lim = limit(a, s, min(i, s.qn - 1));
     const int lim_first = limit(a, s, min(w0, s.qn - 1));
     const int lim_last = limit(a, s, min(w0 + 31, s.qn - 1));
     const int64_t t = s.q0 + min(i, s.qn - 1);
-    const int row0 = threadIdx.x / CPR, col = threadIdx.x % CPR;
-    const bool live = col * 8 < a.dim;
-    if (a.table) load_bias(a, h, bias);
+    const int tid = threadIdx.x;
+    Stage<T, T, DH, NT, BN> st;
+    st.init(tid, a.dim);
+    if (end > 0) st.load(kv, 0, end, a.dim);
+    if (a.table) load_bias(a, h, -(i0 + BM - 1 + s.shift), end - 1 - (i0 + s.shift), bias);
     if (threadIdx.x == 0) first_bad = INT32_MAX;
 
     V8<T> qf[KS], of[KS];
@@ -204,74 +214,43 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
     f32x16 acc[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) acc[db] = zero16();
-    Raw<T> kr[IT], vr[IT];
-    auto fetch = [&](int kb) {
-#pragma unroll
-        for (int n = 0; n < IT; n++) {
-            const int j = kb + row0 + n * (NT / CPR);
-            kr[n] = zero_raw<T>();
-            vr[n] = zero_raw<T>();
-            if (j < end && live) {
-                const Loc at = kv.loc(j);
-                kr[n] = load_raw(kv.k(at) + col * 8, 0);
-                vr[n] = load_raw(kv.v(at) + col * 8, 0);
-            }
-        }
-    };
-    if (AHEAD) fetch(0);
+    if (end > 0) st.put(tiles, tiles + BN * DH);
+    __syncthreads();
+    int buf = 0;
     for (int kb = 0; kb < end; kb += BN) {
-        const bool mixed = min(kb + BN, end) > block_first;
-        if (!AHEAD) fetch(kb);
-        __syncthreads();
-#pragma unroll
-        for (int n = 0; n < IT; n++) {
-            const int row = row0 + n * (NT / CPR);
-            V8<T> x;
-            expand(kr[n], x);
-            if (mixed && clean(x)) atomicMin(&first_bad, kb + row);
-            Tl::put(kt, row, col, x);
-            expand(vr[n], x);
-            Tl::put(vt, row, col, x);
+        T *kt = tiles + buf * 2 * BN * DH, *vt = kt + BN * DH;
+        if (min(kb + BN, end) > block_first) {  // some rows see less of the tile
+            clean_tile<T, DH, NT, BN>(kt, tid, [&](int r) { atomicMin(&first_bad, kb + r); });
+            __syncthreads();
         }
-        __syncthreads();
-        if (AHEAD && kb + BN < end) fetch(kb + BN);
+        const bool more = kb + BN < end;
+        if (NBUF == 2 && more) st.load(kv, kb + BN, end, a.dim);
 #pragma unroll
         for (int n = 0; n < BN / 32; n++) {
-            const int k0 = kb + 32 * n;
+            const int k0 = kb + 32 * n, rel = k0 - (w0 + s.shift);
             if (k0 >= lim_last) break;
             f32x16 x = zero16(), dp = zero16();
 #pragma unroll
             for (int ks = 0; ks < KS; ks++) {
-                x = mma(Tl::rows(kt, 32 * n, ks), qf[ks], x);
-                dp = mma(Tl::rows(vt, 32 * n, ks), of[ks], dp);
+                x = mma(Tl::rows(kt, ln, 32 * n, ks), qf[ks], x);
+                dp = mma(Tl::rows(vt, ln, 32 * n, ks), of[ks], dp);
             }
-            f32x16 f;  // d(score)/d(product), with the scale
-            if (a.capped) {
+            const bool near = a.table && near_block(a, rel);
+            const Scores sc = scores_of<CAP>(a, a.table && !near ? far_bias(a, bias, rel) - lse2 : -lse2, x);
+            x = sc.x;
+            if (near) add_bias(a, bias, rel, x);
 #pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    const float th = tanh_of(a.c1 * x[r]);
-                    x[r] = a.c2 * th;
-                    f[r] = a.scale * __builtin_fmaf(-th, th, 1.0f);
-                }
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    x[r] *= a.c1;
-                    f[r] = a.scale;
-                }
-            }
-            if (a.table) add_bias(a, bias, k0 - (w0 + s.shift), x);
-#pragma unroll
-            for (int r = 0; r < 16; r++) x[r] = exp2_fast(x[r] - lse2) * (dp[r] - delta);
+            for (int r = 0; r < 16; r++) x[r] = exp2_fast(x[r]) * (dp[r] - delta);
             if (k0 + 32 > lim_first) {
                 const int left = lim - k0 - 4 * half;
 #pragma unroll
                 for (int r = 0; r < 16; r++) x[r] = reg_row(r) < left ? x[r] : 0.0f;
             }
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                rest += x[r];
-                x[r] *= f[r];
+            for (int r = 0; r < 16; r++) rest += x[r];
+            if (CAP) {
+#pragma unroll
+                for (int r = 0; r < 16; r++) x[r] *= sc.f[r];
             }
 #pragma unroll
             for (int u = 0; u < 2; u++) {
@@ -279,12 +258,22 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
                 pack(x, u, p);
 #pragma unroll
                 for (int db = 0; db < DB; db++)
-                    acc[db] = mma(Tl::cols(kt, 32 * n + 16 * u, db), p, acc[db]);
+                    acc[db] = mma(Tl::cols(kt, ln, 32 * n + 16 * u, db), p, acc[db]);
             }
         }
+        if (NBUF == 1) {
+            if (more) st.load(kv, kb + BN, end, a.dim);
+            __syncthreads();
+        } else {
+            buf ^= 1;
+        }
+        if (more) {
+            T *next = tiles + buf * 2 * BN * DH;
+            st.put(next, next + BN * DH);
+        }
+        __syncthreads();
     }
     rest += __shfl_xor(rest, 32, kWave);
-    __syncthreads();
     const int bad = first_bad;
     if (bad < lim_last)
         for (int r = 0; r < min(32, s.qn - w0); r++)
@@ -293,7 +282,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
     if (half == 0) g.delta[h * a.total_q + t] = delta + rest;
     T *dp = static_cast<T *>(g.dq.data) + t * g.dq.token_stride + h * g.dq.head_stride;
 #pragma unroll
-    for (int db = 0; db < DB; db++) store_block(dp, acc[db], 1.0f, db, a.dim);
+    for (int db = 0; db < DB; db++) store_block(dp, acc[db], deriv_scale(a), db, a.dim);
 }
 
 // Gradients of the keys and values, and the bias gradient by distance. A
@@ -308,27 +297,27 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
 // keeps one head's and adds them to its own row in the workspace after each.
 // It has all heads that share a key head (span = group), or one (span = 1) and
 // leaves its part of the sum over them to k_attn_sum_heads.
-template <class T, int DH, int NW, int BQ, bool DIST>
+template <class T, bool CAP, int DH, int NW, int BQ, bool DIST, int NBUF>
 __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn_dkv(
     Args a, Grads g, int slots, int span, int kept) {
     typedef Tile<T, DH> Tl;
-    constexpr int BM = NW * 32, NT = NW * 64, CPR = DH / 8, IT = BQ * CPR / NT;
-    constexpr int KS = DH / 16, DB = DH / 32;
-    constexpr bool AHEAD = NW > 1;  // a lone wavefront has no registers for it
+    const typename Tl::Lane ln = Tl::lane();
+    constexpr int BM = NW * 32, NT = NW * 64, KS = DH / 16, DB = DH / 32;
+    // the widest rows leave no registers for the values: they stay in LDS
+    constexpr bool VLDS = sizeof(T) * DH > 256;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int last_bad;
-    __shared__ __attribute__((aligned(16))) float stat[2][BQ];  // lse (in log 2) and delta
-    T *qt = reinterpret_cast<T *>(lds), *ot = qt + BQ * DH;
-    float *bias = reinterpret_cast<float *>(ot + BQ * DH);
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, half = l >> 5;
+    __shared__ __attribute__((aligned(16))) float stat[NBUF][2][BQ];  // lse (in log 2) and delta
+    T *tiles = reinterpret_cast<T *>(lds);  // [NBUF][queries, output gradients][BQ][DH]
+    T *values = tiles + NBUF * 2 * BQ * DH;
+    float *bias = reinterpret_cast<float *>(values + (VLDS ? BM * DH : 0));
+    const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, half = l >> 5;
     const int h0 = blockIdx.y * span, kvh = h0 / a.group, width = 2 * a.reach + 1;
-    float *skew = bias + (a.table ? 2 * (a.reach + kBiasPad) + 1 : 0) + wave * 32 * kSkew;
-    float *dists = skew + (NW - wave) * 32 * kSkew;  // [kept][NW][width]
+    float *skew = bias + (a.table ? 2 * (a.reach + kBiasPad) + 1 : 0) + wave * kSkewFloats;
+    float *dists = skew + (NW - wave) * kSkewFloats;  // [kept][NW][width]
     float far_left = 0.0f, far_right = 0.0f;
     if (DIST)
         for (int d = threadIdx.x; d < kept * NW * width; d += NT) dists[d] = 0.0f;
-    const int row0 = threadIdx.x / CPR, col = threadIdx.x % CPR;
-    const bool live = col * 8 < a.dim;
     // the workgroup's sums of the head in dists + at into its row; with `add`
     // to what the row holds
     auto flush = [&](int h, int at, bool add) {
@@ -342,6 +331,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
         }
     };
     bool begun = false, nan_seen = false;
+    Stage<T, T, DH, NT, BQ> st;
+    st.init(tid, a.dim);
 
     for (int slot = blockIdx.x; slot < slots; slot += int(gridDim.x)) {
     int tile;
@@ -358,7 +349,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     __syncthreads();  // the last tile's flag has been read
     if (threadIdx.x == 0) last_bad = -1;
 
-    V8<T> kf[KS], vf[KS];
+    V8<T> kf[KS], vf[VLDS ? 1 : KS];
+    T *vt = values + wave * 32 * DH;
     {
         const int64_t t = s.k0 + min(j, s.kn - 1);
         const T *kp = static_cast<const T *>(g.k.data) + t * g.k.token_stride + kvh * g.k.head_stride;
@@ -366,98 +358,78 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
 #pragma unroll
         for (int ks = 0; ks < KS; ks++) {
             kf[ks] = chunk_of(kp, 2 * ks + half, a.dim);
-            vf[ks] = chunk_of(vp, 2 * ks + half, a.dim);
+            if (!VLDS) vf[VLDS ? 0 : ks] = chunk_of(vp, 2 * ks + half, a.dim);
+        }
+        if (VLDS) {  // the wavefront's own; read after the barriers below
+#pragma unroll
+            for (int ks = 0; ks < KS; ks++)
+                Tl::put(vt, l & 31, 2 * ks + half, chunk_of(vp, 2 * ks + half, a.dim));
         }
     }
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) dk[db] = dv[db] = zero16();
 
-    Raw<T> qr[IT], gr[IT];
     float lse_r = 0.0f, delta_r = 0.0f;
     auto fetch = [&](int h, int qb) {
-#pragma unroll
-        for (int n = 0; n < IT; n++) {
-            const int i = qb + row0 + n * (NT / CPR);
-            qr[n] = zero_raw<T>();
-            gr[n] = zero_raw<T>();
-            if (i < s.qn && live) {
-                const int64_t t = s.q0 + i;
-                qr[n] = load_raw(static_cast<const T *>(g.q.data) + t * g.q.token_stride +
-                                     h * g.q.head_stride + col * 8, 0);
-                gr[n] = load_raw(static_cast<const T *>(g.grad_out.data) +
-                                     t * g.grad_out.token_stride + h * g.grad_out.head_stride +
-                                     col * 8, 0);
-            }
-        }
-        if (threadIdx.x < BQ) {
-            const int i = qb + int(threadIdx.x);
-            const bool in = i < s.qn;  // queries past the last one: probability 0
-            lse_r = in ? g.lse[h * a.total_q + s.q0 + i] * kLog2e : INFINITY;
-            delta_r = in ? g.delta[h * a.total_q + s.q0 + i] : 0.0f;
+        st.load_rows(static_cast<const T *>(g.q.data) + s.q0 * g.q.token_stride + h * g.q.head_stride,
+                     static_cast<const T *>(g.grad_out.data) + s.q0 * g.grad_out.token_stride +
+                         h * g.grad_out.head_stride,
+                     g.q.token_stride, g.grad_out.token_stride, qb, s.qn - 1);
+        const int64_t t = h * a.total_q + s.q0 + min(qb + (tid & (BQ - 1)), s.qn - 1);
+        lse_r = g.lse[t] * kLog2e;
+        delta_r = g.delta[t];
+    };
+    auto put = [&](int n) {
+        T *p = tiles + n * 2 * BQ * DH;
+        st.put(p, p + BQ * DH);
+        if (tid < BQ) {
+            stat[n][0][tid] = lse_r;
+            stat[n][1][tid] = delta_r;
         }
     };
     for (int hg = 0; hg < span; hg++) {
         const int h = h0 + hg;
-        if (AHEAD && begin < s.qn) fetch(h, begin);
-        if (a.table) {
-            __syncthreads();
-            load_bias(a, h, bias);
-        }
         float *dist = dists + ((kept > 1 ? hg : 0) * NW + wave) * width;
+        if (begin < s.qn) fetch(h, begin);
+        __syncthreads();  // the last head's tiles and bias have been read
+        if (a.table) load_bias(a, h, j0 - (s.qn - 1 + s.shift), j0 + BM - 1 - (begin + s.shift), bias);
+        if (begin < s.qn) put(0);
+        __syncthreads();
+        int buf = 0;
         for (int qb = begin; qb < s.qn; qb += BQ) {
-            const bool mixed = qb < block_last;
-            if (!AHEAD) fetch(h, qb);
-            __syncthreads();
-#pragma unroll
-            for (int n = 0; n < IT; n++) {
-                const int row = row0 + n * (NT / CPR);
-                V8<T> x, y;
-                expand(qr[n], x);
-                expand(gr[n], y);
-                if (mixed) {
-                    const bool bx = clean(x), by = clean(y);
-                    if (bx || by) atomicMax(&last_bad, qb + row);
-                }
-                Tl::put(qt, row, col, x);
-                Tl::put(ot, row, col, y);
+            T *qt = tiles + buf * 2 * BQ * DH, *ot = qt + BQ * DH;
+            if (qb < block_last) {  // some keys are not seen by all of the tile
+                const auto seen = [&](int r) { atomicMax(&last_bad, min(qb + r, s.qn - 1)); };
+                clean_tile<T, DH, NT, BQ>(qt, tid, seen);
+                clean_tile<T, DH, NT, BQ>(ot, tid, seen);
+                __syncthreads();
             }
-            if (threadIdx.x < BQ) {
-                stat[0][threadIdx.x] = lse_r;
-                stat[1][threadIdx.x] = delta_r;
-            }
-            __syncthreads();
-            if (AHEAD && qb + BQ < s.qn) fetch(h, qb + BQ);
+            const bool more = qb + BQ < s.qn;
+            if (NBUF == 2 && more) fetch(h, qb + BQ);
+            const int now = buf;
 #pragma unroll
             for (int n = 0; n < BQ / 32; n++) {
                 const int q0 = qb + 32 * n;
-                if (q0 + 32 <= fq_first || q0 >= s.qn) continue;
+                if (q0 + 32 <= fq_first || q0 >= s.qn) continue;  // (uniform)
+                const int rel = w0 - (q0 + s.shift);
                 f32x16 x = zero16(), dp = zero16();
 #pragma unroll
                 for (int ks = 0; ks < KS; ks++) {
-                    x = mma(Tl::rows(qt, 32 * n, ks), kf[ks], x);
-                    dp = mma(Tl::rows(ot, 32 * n, ks), vf[ks], dp);
+                    x = mma(Tl::rows(qt, ln, 32 * n, ks), kf[ks], x);
+                    dp = mma(Tl::rows(ot, ln, 32 * n, ks),
+                             VLDS ? Tl::rows(vt, ln, 0, ks) : vf[VLDS ? 0 : ks], dp);
                 }
-                f32x16 f;
-                if (a.capped) {
-#pragma unroll
-                    for (int r = 0; r < 16; r++) {
-                        const float th = tanh_of(a.c1 * x[r]);
-                        x[r] = a.c2 * th;
-                        f[r] = a.scale * __builtin_fmaf(-th, th, 1.0f);
-                    }
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 16; r++) {
-                        x[r] *= a.c1;
-                        f[r] = a.scale;
-                    }
-                }
-                if (a.table) add_bias_queries(a, bias, w0 - (q0 + s.shift), x);
+                const bool near = a.table && near_block(a, rel);
+                const Scores sc = scores_of<CAP>(a, a.table && !near ? far_bias(a, bias, rel) : 0.0f, x);
+                x = sc.x;
+                if (near) add_bias_queries(a, bias, rel, x);
 #pragma unroll
                 for (int c = 0; c < 4; c++) {
-                    const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stat[0][32 * n + 8 * c + 4 * half]);
-                    const f32x4 del = *reinterpret_cast<const f32x4 *>(&stat[1][32 * n + 8 * c + 4 * half]);
+                    const f32x4 lse = *reinterpret_cast<const f32x4 *>(
+                        &stat[now][0][32 * n + 8 * c + 4 * half]);
+                    const f32x4 del = *reinterpret_cast<const f32x4 *>(
+                        &stat[now][1][32 * n + 8 * c + 4 * half]);
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
                         const int r = 4 * c + e;
@@ -465,12 +437,13 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
                         dp[r] = x[r] * (dp[r] - del[e]);
                     }
                 }
-                if (q0 < fq_last) {
-                    const int from = fq - q0 - 4 * half;
+                if (q0 < fq_last || q0 + 32 > s.qn) {  // queries that see the key, up to the last
+                    const int from = fq - q0 - 4 * half, to = s.qn - q0 - 4 * half;
 #pragma unroll
                     for (int r = 0; r < 16; r++) {
-                        x[r] = reg_row(r) >= from ? x[r] : 0.0f;
-                        dp[r] = reg_row(r) >= from ? dp[r] : 0.0f;
+                        const bool in = reg_row(r) >= from && reg_row(r) < to;
+                        x[r] = in ? x[r] : 0.0f;
+                        dp[r] = in ? dp[r] : 0.0f;
                     }
                 }
                 if (DIST) {
@@ -478,10 +451,12 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
 #pragma unroll
                         for (int r = 0; r < 16; r++) dp[r] = j < s.kn ? dp[r] : 0.0f;
                     }
-                    add_distances(a, dp, w0 - (q0 + s.shift), skew, dist, far_left, far_right);
+                    add_distances(a, dp, rel, skew, dist, far_left, far_right);
                 }
+                if (CAP) {
 #pragma unroll
-                for (int r = 0; r < 16; r++) dp[r] *= f[r];
+                    for (int r = 0; r < 16; r++) dp[r] *= sc.f[r];
+                }
 #pragma unroll
                 for (int u = 0; u < 2; u++) {
                     V8<T> p, d;
@@ -489,11 +464,19 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
                     pack(dp, u, d);
 #pragma unroll
                     for (int db = 0; db < DB; db++) {
-                        dv[db] = mma(Tl::cols(ot, 32 * n + 16 * u, db), p, dv[db]);
-                        dk[db] = mma(Tl::cols(qt, 32 * n + 16 * u, db), d, dk[db]);
+                        dv[db] = mma(Tl::cols(ot, ln, 32 * n + 16 * u, db), p, dv[db]);
+                        dk[db] = mma(Tl::cols(qt, ln, 32 * n + 16 * u, db), d, dk[db]);
                     }
                 }
             }
+            if (NBUF == 1) {
+                if (more) fetch(h, qb + BQ);
+                __syncthreads();
+            } else {
+                buf ^= 1;
+            }
+            if (more) put(buf);
+            __syncthreads();
         }
         if (DIST) {
             far_left = wave_sum(far_left);
@@ -526,7 +509,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
             float *vp = kp + int64_t(a.heads) * g.total_k * a.dim;
 #pragma unroll
             for (int db = 0; db < DB; db++) {
-                store_block(kp, dk[db], 1.0f, db, a.dim);
+                store_block(kp, dk[db], deriv_scale(a), db, a.dim);
                 store_block(vp, dv[db], 1.0f, db, a.dim);
             }
         } else {
@@ -534,7 +517,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
             T *vp = static_cast<T *>(g.dv.data) + t * g.dv.token_stride + kvh * g.dv.head_stride;
 #pragma unroll
             for (int db = 0; db < DB; db++) {
-                store_block(kp, dk[db], 1.0f, db, a.dim);
+                store_block(kp, dk[db], deriv_scale(a), db, a.dim);
                 store_block(vp, dv[db], 1.0f, db, a.dim);
             }
         }
@@ -578,31 +561,60 @@ __global__ __launch_bounds__(kBlock) void k_attn_sum_heads(Args a, Grads g) {
     }
 }
 
-// Sums the parts of every (head, distance), in order, into part 0.
+// Sums every kBiasRun parts of a (head, distance), in order, into the first.
+constexpr int kBiasRun = 64;
 __global__ __launch_bounds__(kBlock) void k_bias_parts(float *part, int parts, int width) {
     __shared__ float sum[4][kWave];
-    const int d = blockIdx.x * kWave + threadIdx.x % kWave, w = threadIdx.x / kWave;
-    float *p = part + int64_t(blockIdx.y) * parts * width;
+    const int l = threadIdx.x % kWave, w = threadIdx.x / kWave;
+    const int d = blockIdx.x * kWave + l, first = blockIdx.z * kBiasRun;
+    float *p = part + (int64_t(blockIdx.y) * parts + first) * width;
+    const int n = min(kBiasRun, parts - first);
     float x = 0.0f;
-    if (d < width)
-        for (int i = w; i < parts; i += 4) x += p[int64_t(i) * width + d];
-    sum[w][threadIdx.x % kWave] = x;
-    __syncthreads();
-    if (w == 0 && d < width) {
-        const int l = threadIdx.x;
-        p[d] = (sum[0][l] + sum[1][l]) + (sum[2][l] + sum[3][l]);
+    if (d < width) {
+#pragma unroll 8
+        for (int i = w; i < n; i += 4) x += p[int64_t(i) * width + d];
     }
+    sum[w][l] = x;
+    __syncthreads();
+    if (w == 0 && d < width) p[d] = (sum[0][l] + sum[1][l]) + (sum[2][l] + sum[3][l]);
 }
 
-// Sums the distances of every (bucket, head), in order: a wavefront each.
-__global__ __launch_bounds__(kWave) void k_bias_buckets(Args a, const float *part, int parts,
-                                                        int width, float *grad) {
+// Sums the distances of every (bucket, head) over every step-th part, in a fixed
+// order: a workgroup each, whose lanes first list the bucket's distances.
+__global__ __launch_bounds__(kBlock) void k_bias_buckets(Args a, const float *part, int parts,
+                                                         int step, int width, float *grad) {
+    __shared__ int list[2 * kMaxReach + 1];
+    __shared__ int count[kBlock / kWave];
+    __shared__ float sum[kBlock / kWave];
+    const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
+    // distances in order: a wavefront's share of them, after those before it
+    const int share = (width + 3) / 4, d0 = w * share, d1 = min(d0 + share, width);
+    int n = 0;
+    for (int pass = 0; pass < 2; pass++) {
+        int at = 0;
+        if (pass)
+            for (int k = 0; k < w; k++) at += count[k];
+        for (int d = d0; d < d1; d += kWave) {
+            const bool mine = d + l < d1 && a.bucket_of[d + l] == int(blockIdx.x);
+            const uint64_t m = __ballot(mine);
+            if (pass && mine) list[at + __popcll(m & ((uint64_t(1) << l) - 1))] = d + l;
+            at += __popcll(m);
+        }
+        if (!pass && l == 0) count[w] = at;
+        __syncthreads();
+    }
+    n = count[0] + count[1] + count[2] + count[3];
     const float *p = part + int64_t(blockIdx.y) * parts * width;
+    const int runs = (parts + step - 1) / step;
     float x = 0.0f;
-    for (int d = threadIdx.x; d < width; d += kWave)
-        if (a.bucket_of[d] == int(blockIdx.x)) x += p[d];
+#pragma unroll 4
+    for (int i = tid; i < n * runs; i += kBlock)
+        x += p[int64_t(i / n) * step * width + list[i % n]];
     x = wave_sum(x);
-    if (threadIdx.x == 0) grad[int64_t(blockIdx.x) * a.heads + blockIdx.y] = x;
+    if (l == 0) sum[w] = x;
+    __syncthreads();
+    if (tid == 0)
+        grad[int64_t(blockIdx.x) * a.heads + blockIdx.y] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
 // Tiles and workgroups of a call, from its sizes alone.
@@ -651,38 +663,39 @@ Space space_of(const tc_attn &a) {
     return s;
 }
 
-template <class T, int DH, int NW, bool DIST>
+template <class T, bool CAP, int DH, int NW, bool DIST>
 void launch_dkv(const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
+    constexpr int NBUF = NW == 1 ? 1 : 2;
     const size_t width = DIST ? (2 * a.reach + 1) * sizeof(float) : 0;
     // sums by distance of all heads of a workgroup in 32 KB, or of one
     const int kept = size_t(p.span) * NW * width <= (32 << 10) ? p.span : 1;
-    const size_t bytes = 2 * 32 * DH * sizeof(T) +
+    const size_t bytes = (NBUF * 2 * 32 + (sizeof(T) * DH > 256 ? NW * 32 : 0)) * DH * sizeof(T) +
                          (a.table ? bias_entries(a.reach) * sizeof(float) : 0) +
-                         (DIST ? NW * 32 * kSkew * sizeof(float) : 0) + kept * NW * width;
-    hipLaunchKernelGGL((k_attn_dkv<T, DH, NW, 32, DIST>), dim3(p.parts, a.heads / p.span),
+                         (DIST ? NW * kSkewFloats * sizeof(float) : 0) + kept * NW * width;
+    hipLaunchKernelGGL((k_attn_dkv<T, CAP, DH, NW, 32, DIST, NBUF>), dim3(p.parts, a.heads / p.span),
                        dim3(NW * 64), bytes, stream, a, g, int(p.k_slots), p.span, kept);
 }
 
-template <class T, int DH>
+template <class T, bool CAP, int DH>
 void launch(const tc_attn &t, const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
     constexpr int BN = sizeof(T) == 4 ? 32 : 64;
     const size_t bias = a.table ? bias_entries(a.reach) * sizeof(float) : 0;
     if (t.total_q > 0) {
         const dim3 grid(unsigned(p.q_slots * a.heads));
         if (p.q_waves == 1)
-            hipLaunchKernelGGL((k_attn_dq<T, DH, 1, 32>), grid, dim3(64),
+            hipLaunchKernelGGL((k_attn_dq<T, CAP, DH, 1, 32, 1>), grid, dim3(64),
                                2 * 32 * DH * sizeof(T) + bias, stream, a, g, int(p.q_slots));
         else
-            hipLaunchKernelGGL((k_attn_dq<T, DH, 4, BN>), grid, dim3(256),
-                               2 * BN * DH * sizeof(T) + bias, stream, a, g, int(p.q_slots));
+            hipLaunchKernelGGL((k_attn_dq<T, CAP, DH, 4, BN, 2>), grid, dim3(256),
+                               4 * BN * DH * sizeof(T) + bias, stream, a, g, int(p.q_slots));
     }
     if (t.total_k > 0) {
         if (p.k_waves == 1)
-            g.bias_part ? launch_dkv<T, DH, 1, true>(a, p, g, stream)
-                        : launch_dkv<T, DH, 1, false>(a, p, g, stream);
+            g.bias_part ? launch_dkv<T, CAP, DH, 1, true>(a, p, g, stream)
+                        : launch_dkv<T, CAP, DH, 1, false>(a, p, g, stream);
         else
-            g.bias_part ? launch_dkv<T, DH, 4, true>(a, p, g, stream)
-                        : launch_dkv<T, DH, 4, false>(a, p, g, stream);
+            g.bias_part ? launch_dkv<T, CAP, DH, 4, true>(a, p, g, stream)
+                        : launch_dkv<T, CAP, DH, 4, false>(a, p, g, stream);
         if (g.part) {
             const int64_t n = 2 * t.total_k * t.num_kv_heads * (t.head_dim / 4);
             hipLaunchKernelGGL((k_attn_sum_heads<T>),
@@ -694,20 +707,25 @@ void launch(const tc_attn &t, const Args &a, const Plan &p, const Grads &g, hipS
 
 void backward(const tc_attn &p, const Plan &plan, const Args &a, const Grads &g, float *grad_bias,
               hipStream_t stream) {
+#define TC_LAUNCH(T, CAP)                                              \
+    (p.head_dim <= 64 ? launch<T, CAP, 64>(p, a, plan, g, stream)      \
+                      : launch<T, CAP, 128>(p, a, plan, g, stream))
     if (p.dtype == TC_F32)
-        p.head_dim <= 64 ? launch<float, 64>(p, a, plan, g, stream)
-                         : launch<float, 128>(p, a, plan, g, stream);
+        a.capped ? TC_LAUNCH(float, true) : TC_LAUNCH(float, false);
     else
-        p.head_dim <= 64 ? launch<bf16, 64>(p, a, plan, g, stream)
-                         : launch<bf16, 128>(p, a, plan, g, stream);
+        a.capped ? TC_LAUNCH(bf16, true) : TC_LAUNCH(bf16, false);
+#undef TC_LAUNCH
     if (!grad_bias) return;
     // without queries or keys there are no parts, and every sum is 0
     const int width = p.total_q > 0 && p.total_k > 0 ? 2 * a.reach + 1 : 0;
-    if (width > 0)
-        hipLaunchKernelGGL(k_bias_parts, dim3((width + 63) / 64, a.heads), dim3(kBlock), 0, stream,
-                           g.bias_part, plan.parts, width);
-    hipLaunchKernelGGL(k_bias_buckets, dim3(p.num_buckets, a.heads), dim3(kWave), 0, stream, a,
-                       g.bias_part, plan.parts, width, grad_bias);
+    // parts are summed in runs first where there are many
+    const int step = plan.parts > 8 * kBiasRun ? kBiasRun : 1;
+    if (width > 0 && step > 1)
+        hipLaunchKernelGGL(k_bias_parts, dim3((width + 63) / 64, a.heads,
+                                              (plan.parts + kBiasRun - 1) / kBiasRun),
+                           dim3(kBlock), 0, stream, g.bias_part, plan.parts, width);
+    hipLaunchKernelGGL(k_bias_buckets, dim3(p.num_buckets, a.heads), dim3(kBlock), 0, stream, a,
+                       g.bias_part, plan.parts, step, width, grad_bias);
 }
 
 }  // namespace

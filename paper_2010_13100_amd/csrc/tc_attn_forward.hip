@@ -25,6 +25,12 @@ struct Output {
 
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
+// Weight of a split with maximum m and sum `sum` where the row's maximum is
+// `top`; a split of scores -inf weighs nothing, one with a NaN is NaN.
+__device__ __forceinline__ float split_weight(float m, float sum, float top) {
+    return m == -INFINITY ? (sum == 0.0f ? 0.0f : sum) : exp2_fast(m - top);
+}
+
 __device__ __forceinline__ float log_sum(float m, float l) {
     return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
@@ -59,19 +65,37 @@ __device__ void finish_row(const Args &a, const Seq &s, const KV &kv, tc_rows q,
     }
 }
 
+// Wavefronts of k_attn_tile on a SIMD that its registers are cut to, and the
+// keys of its tiles. Products, exponentials and LDS reads of a tile depend on
+// one another in turn, so wavefronts on a SIMD count more than anything within
+// one: 2 x 8192 causal queries of 16 heads of 128 bf16 take 745 us with three and
+// tiles of 32 keys, 803 with two and tiles of 64, 895 with two and a branch-free
+// path for the tiles that need no mask or bias (more registers). Heads of 64
+// take 526 us with tiles of 64 and no cut, 571 to 584 with three to five.
+template <class T>
+constexpr int tile_waves(int dh, int nw) {
+    if (sizeof(T) == 2 && dh > 64 && nw > 1) return 3;
+    return sizeof(T) * dh <= 256 ? 2 : 1;
+}
+template <class T>
+constexpr int tile_keys(int dh) {
+    return sizeof(T) == 2 && dh <= 64 ? 64 : 32;
+}
+
 // Attention of NW*32 queries of one head: a wavefront has 32 queries, the
-// workgroup shares tiles of BN keys and values in LDS.
-template <class T, class CT, bool PAGED, int DH, int NW, int BN>
-__global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_tile(Args a, Source src, tc_rows q, Output<T> o,
-                                                       Split sp, int slots) {
+// workgroup shares tiles of BN keys and values in LDS. With NBUF = 2 the next
+// tile arrives while this one is worked on; a lone wavefront, whose share of a
+// tile is four times as large, has no registers for that.
+template <class T, class CT, bool PAGED, bool CAP, int DH, int NW, int BN, int NBUF>
+__global__ __launch_bounds__(NW * 64, tile_waves<T>(DH, NW)) void k_attn_tile(
+    Args a, Source src, tc_rows q, Output<T> o, Split sp, int slots) {
     typedef Tile<T, DH> Tl;
-    constexpr int BM = NW * 32, NT = NW * 64, CPR = DH / 8, IT = BN * CPR / NT;
-    constexpr bool AHEAD = NW > 1;  // a lone wavefront has no registers for it
-    static_assert(BN * CPR % NT == 0 && NT % CPR == 0, "");
+    const typename Tl::Lane ln = Tl::lane();
+    constexpr int BM = NW * 32, NT = NW * 64, NB = BN / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int first_bad;  // first key whose value was cleaned
-    T *kt = reinterpret_cast<T *>(lds), *vt = kt + BN * DH;
-    float *bias = reinterpret_cast<float *>(vt + BN * DH);
+    T *tiles = reinterpret_cast<T *>(lds);  // [NBUF][keys, values][BN][DH]
+    float *bias = reinterpret_cast<float *>(tiles + NBUF * 2 * BN * DH);
 
     // heads that share keys run on the same XCD (workgroups go round them);
     // a sequence's last tiles, which see the most keys, come first
@@ -88,12 +112,18 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
     if (split > 0 && j0 >= seen) return;
     const auto kv = KvOf<CT, PAGED>::make(src, s, kvh);
 
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, half = l >> 5;
+    const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, half = l >> 5;
+    Stage<T, CT, DH, NT, BN> st;
+    st.init(tid, a.dim);
+    st.look_up(kv, j0, end);
+    if (j0 < end) st.load(kv, j0, end, a.dim);
+    st.look_up(kv, j0 + BN, end);
+
     const int w0 = i0 + wave * 32, i = w0 + (l & 31);
     const int lim = limit(a, s, min(i, s.qn - 1));
     const int lim_first = limit(a, s, min(w0, s.qn - 1)), lim_last = limit(a, s, min(w0 + 31, s.qn - 1));
     const int block_first = limit(a, s, i0);
-    if (a.table) load_bias(a, h, bias);
+    if (a.table) load_bias(a, h, j0 - (i0 + BM - 1 + s.shift), end - 1 - (i0 + s.shift), bias);
     if (threadIdx.x == 0) first_bad = INT32_MAX;
 
     V8<T> qf[DH / 16];
@@ -103,92 +133,51 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
 #pragma unroll
         for (int ks = 0; ks < DH / 16; ks++) qf[ks] = chunk_of(qp, 2 * ks + half, a.dim);
     }
-
     f32x16 acc[DH / 32];
 #pragma unroll
     for (int db = 0; db < DH / 32; db++) acc[db] = zero16();
-    float m = -INFINITY, sum = 0.0f;
+    Softmax sm;
 
-    const int row0 = threadIdx.x / CPR, col = threadIdx.x % CPR;
-    const bool live = col * 8 < a.dim;
-    Raw<CT> kr[IT], vr[IT];
-    auto fetch = [&](int kb) {
-#pragma unroll
-        for (int n = 0; n < IT; n++) {
-            const int j = kb + row0 + n * (NT / CPR);
-            kr[n] = zero_raw<CT>();
-            vr[n] = zero_raw<CT>();
-            if (j < end && live) {
-                const Loc at = kv.loc(j);
-                kr[n] = load_raw(kv.k(at) + col * 8, kv.k_exp(at));
-                vr[n] = load_raw(kv.v(at) + col * 8, kv.v_exp(at));
-            }
-        }
-    };
-    if (AHEAD) fetch(j0);
-    for (int kb = j0; kb < end; kb += BN) {
-        const bool mixed = min(kb + BN, end) > block_first;  // some rows see less of the tile
-        if (!AHEAD) fetch(kb);
-        __syncthreads();
-#pragma unroll
-        for (int n = 0; n < IT; n++) {
-            const int row = row0 + n * (NT / CPR);
-            V8<T> x;
-            expand(kr[n], x);
-            Tl::put(kt, row, col, x);
-            expand(vr[n], x);
-            if (mixed && clean(x)) atomicMin(&first_bad, kb + row);
-            Tl::put(vt, row, col, x);
-        }
-        __syncthreads();
-        if (AHEAD && kb + BN < end) fetch(kb + BN);
-        if (kb >= lim_last) continue;
-
-        f32x16 x[BN / 32];
+    auto work = [&](int kb, const T *kt, const T *vt) {
+        f32x16 x[NB];
         float top = -INFINITY;
 #pragma unroll
-        for (int n = 0; n < BN / 32; n++) {
-            const int k0 = kb + 32 * n;
-            x[n] = zero16();
+        for (int n = 0; n < NB; n++) x[n] = zero16();
 #pragma unroll
-            for (int ks = 0; ks < DH / 16; ks++) x[n] = mma(Tl::rows(kt, 32 * n, ks), qf[ks], x[n]);
-            if (a.capped) {
+        for (int ks = 0; ks < DH / 16; ks++)
 #pragma unroll
-                for (int r = 0; r < 16; r++) x[n][r] = a.c2 * tanh_of(a.c1 * x[n][r]);
-            } else {
+            for (int n = 0; n < NB; n++) x[n] = mma(Tl::rows(kt, ln, 32 * n, ks), qf[ks], x[n]);
 #pragma unroll
-                for (int r = 0; r < 16; r++) x[n][r] *= a.c1;
-            }
-            if (a.table) add_bias(a, bias, k0 - (w0 + s.shift), x[n]);
+        for (int n = 0; n < NB; n++) {
+            const int k0 = kb + 32 * n, rel = k0 - (w0 + s.shift);
+            const bool near = a.table && near_block(a, rel);
+            to_scores<CAP>(a, a.table && !near ? far_bias(a, bias, rel) - sm.ref : -sm.ref, x[n]);
+            if (near) add_bias(a, bias, rel, x[n]);
             if (k0 + 32 > lim_first || k0 + 32 > end) {
                 const int left = min(lim, end) - k0 - 4 * half;
 #pragma unroll
-                for (int r = 0; r < 16; r++)
-                    x[n][r] = reg_row(r) < left ? x[n][r] : -INFINITY;
+                for (int r = 0; r < 16; r++) x[n][r] = reg_row(r) < left ? x[n][r] : -INFINITY;
             }
 #pragma unroll
-            for (int r = 0; r < 16; r++) top = fmaxf(top, x[n][r]);
+            for (int r = 0; r < 16; r += 2) top = max3(top, x[n][r], x[n][r + 1]);
         }
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        // the subtracted value need not be the maximum, only near it: it moves
-        // when a score passes it by 2^8, which costs nothing in fp32 sums
-        if (__any(top > m + 8.0f)) {
-            const float next = fmaxf(m, top);
-            const float keep = next == -INFINITY ? 1.0f : exp2_fast(m - next);
-            m = next;
-            sum *= keep;
+        float d, keep;
+        if (sm.moves(top, d, keep)) {
 #pragma unroll
             for (int db = 0; db < DH / 32; db++)
 #pragma unroll
                 for (int r = 0; r < 16; r++) acc[db][r] *= keep;
-        }
-        const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-        for (int n = 0; n < BN / 32; n++) {
+            for (int n = 0; n < NB; n++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) x[n][r] -= d;
+        }
+#pragma unroll
+        for (int n = 0; n < NB; n++) {
 #pragma unroll
             for (int r = 0; r < 16; r++) {
-                x[n][r] = exp2_fast(x[n][r] - base);
-                sum += x[n][r];
+                x[n][r] = exp2_fast(x[n][r]);
+                sm.sum += x[n][r];
             }
 #pragma unroll
             for (int u = 0; u < 2; u++) {
@@ -196,13 +185,43 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
                 pack(x[n], u, p);
 #pragma unroll
                 for (int db = 0; db < DH / 32; db++)
-                    acc[db] = mma(Tl::cols(vt, 32 * n + 16 * u, db), p, acc[db]);
+                    acc[db] = mma(Tl::cols(vt, ln, 32 * n + 16 * u, db), p, acc[db]);
             }
         }
+    };
+
+    if (j0 < end) st.put(tiles, tiles + BN * DH);
+    __syncthreads();
+    int buf = 0;
+    for (int kb = j0; kb < end; kb += BN) {
+        T *kt = tiles + buf * 2 * BN * DH, *vt = kt + BN * DH;
+        if (min(kb + BN, end) > block_first) {  // some rows see less of the tile
+            clean_tile<T, DH, NT, BN>(vt, tid, [&](int r) { atomicMin(&first_bad, kb + r); });
+            __syncthreads();
+        }
+        const bool more = kb + BN < end;
+        if (NBUF == 2 && more) {
+            st.load(kv, kb + BN, end, a.dim);
+            st.look_up(kv, kb + 2 * BN, end);
+        }
+        if (kb < lim_last) work(kb, kt, vt);
+        if (NBUF == 1) {
+            if (more) {
+                st.load(kv, kb + BN, end, a.dim);
+                st.look_up(kv, kb + 2 * BN, end);
+            }
+            __syncthreads();
+        } else {
+            buf ^= 1;
+        }
+        if (more) {
+            T *next = tiles + buf * 2 * BN * DH;
+            st.put(next, next + BN * DH);
+        }
+        __syncthreads();
     }
 
-    sum += __shfl_xor(sum, 32, kWave);
-    __syncthreads();
+    sm.finish();
     const int bad = first_bad;
     if (bad < lim_last)
         for (int r = 0; r < min(32, s.qn - w0); r++)
@@ -211,18 +230,18 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
     const int64_t t = s.q0 + i, row = t * a.heads + h;
     if (sp.chunk == 0 || lim <= sp.chunk) {
         if (split > 0) return;
-        const float inv = inverse(sum);
+        const float inv = inverse(sm.sum);
         T *op = static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride;
 #pragma unroll
         for (int db = 0; db < DH / 32; db++) store_block(op, acc[db], inv, db, a.dim);
-        if (o.lse && half == 0) o.lse[h * a.total_q + t] = log_sum(m, sum);
+        if (o.lse && half == 0) o.lse[h * a.total_q + t] = log_sum(sm.ref, sm.sum);
     } else if (j0 < lim) {
         const int64_t at = split * a.total_q * a.heads + row;
 #pragma unroll
         for (int db = 0; db < DH / 32; db++) store_block(sp.o + at * a.dim, acc[db], 1.0f, db, a.dim);
         if (half == 0) {
-            sp.ml[2 * at] = m;
-            sp.ml[2 * at + 1] = sum;
+            sp.ml[2 * at] = sm.ref;
+            sp.ml[2 * at + 1] = sm.sum;
         }
     }
 }
@@ -230,19 +249,19 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
 // Attention of a few queries over many keys (decoding): the queries of all
 // heads that share a key head are the 32 columns of one block, row r being
 // query r / group, head r % group. Each wavefront takes every fourth block of
-// 32 keys for itself, so that nothing waits for another wavefront before the
-// end; keys go from memory to the operands directly (a lane reads row l%32),
-// values through a tile of the wavefront's own.
+// 32 keys for itself, with tiles of its own, so that nothing waits for another
+// wavefront before the end; the next block arrives while one is worked on.
 template <class T, class CT, bool PAGED, int DH>
 __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_few(Args a, Source src, tc_rows q, Output<T> o,
                                                      Split sp, int row_tiles) {
     typedef Tile<T, DH> Tl;
+    const typename Tl::Lane ln = Tl::lane();
     constexpr int KS = DH / 16, DB = DH / 32, NW = kBlock / 64;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ float stat[NW][2][32];
     __shared__ int first_bad;
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, half = l >> 5;
-    T *vt = reinterpret_cast<T *>(lds) + wave * 32 * DH;
+    T *kt = reinterpret_cast<T *>(lds) + wave * 2 * 32 * DH, *vt = kt + 32 * DH;  // its own
 
     int id = blockIdx.x;
     const int kvh = id % a.kv_heads;
@@ -275,77 +294,44 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
     f32x16 acc[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) acc[db] = zero16();
-    float m = -INFINITY, sum = 0.0f;
+    Softmax sm;
 
-    Raw<CT> kr[KS], vr[KS];
-    Loc next{};
-    auto locate = [&](int kb) {  // keys past the end repeat the last one
-        if (kb < end) next = kv.loc(min(kb + (l & 31), end - 1));
-    };
-    auto fetch_k = [&](const Loc &at) {
-        const uint32_t e = kv.k_exp(at);
-#pragma unroll
-        for (int ks = 0; ks < KS; ks++)
-            kr[ks] = (2 * ks + half) * 8 < a.dim ? load_raw(kv.k(at) + (2 * ks + half) * 8, e)
-                                                 : zero_raw<CT>();
-    };
-    auto fetch_v = [&](const Loc &at, bool held) {
-        const uint32_t e = kv.v_exp(at);
-#pragma unroll
-        for (int ks = 0; ks < KS; ks++)
-            vr[ks] = held && (2 * ks + half) * 8 < a.dim
-                         ? load_raw(kv.v(at) + (2 * ks + half) * 8, e)
-                         : zero_raw<CT>();
-    };
     constexpr int STEP = 32 * NW;
+    Stage<T, CT, DH, 64, 32> st;
+    st.init(l, a.dim);
     int kb = j0 + wave * 32;
-    locate(kb);
-    if (kb < end) {
-        fetch_k(next);
-        fetch_v(next, kb + (l & 31) < end);
-    }
-    locate(kb + STEP);
+    st.look_up(kv, kb, end);
+    if (kb < end) st.load(kv, kb, end, a.dim);
+    st.look_up(kv, kb + STEP, end);
     for (; kb < end; kb += STEP) {
+        st.put(kt, vt);
+        if (kb + STEP < end) {
+            st.load(kv, kb + STEP, end, a.dim);
+            st.look_up(kv, kb + 2 * STEP, end);
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (min(kb + 32, end) > seen_first) {  // some rows see less of the block
+            clean_tile<T, DH, 64, 32>(vt, l, [&](int r) { atomicMin(&first_bad, kb + r); });
+            __builtin_amdgcn_wave_barrier();
+        }
         f32x16 x = zero16();
 #pragma unroll
-        for (int ks = 0; ks < KS; ks++) {
-            V8<T> k8;
-            expand(kr[ks], k8);
-            x = mma(k8, qf[ks], x);
-        }
-        const Loc at = next;
-        const bool more = kb + STEP < end;
-        if (more) fetch_k(at);
-        const bool mixed = min(kb + 32, end) > seen_first;
-#pragma unroll
-        for (int ks = 0; ks < KS; ks++) {
-            V8<T> v8;
-            expand(vr[ks], v8);
-            if (mixed && clean(v8)) atomicMin(&first_bad, kb + (l & 31));
-            Tl::put(vt, l & 31, 2 * ks + half, v8);
-        }
-        if (more) fetch_v(at, kb + STEP + (l & 31) < end);
-        locate(kb + 2 * STEP);
+        for (int ks = 0; ks < KS; ks++) x = mma(Tl::rows(kt, ln, 0, ks), qf[ks], x);
 
-        if (a.capped) {
+        // distances of the block, over its queries
+        const int lo = kb - (i_last + s.shift), hi = kb + 31 - (i_first + s.shift);
+        const bool near = a.table && hi > -a.reach && lo < a.reach;
+        const float c0 = a.table && !near ? (hi <= -a.reach ? far_left : far_right) - sm.ref : -sm.ref;
+        if (a.capped)
+            to_scores<true>(a, c0, x);
+        else
+            to_scores<false>(a, c0, x);
+        if (near) {
+            float y[16];
 #pragma unroll
-            for (int r = 0; r < 16; r++) x[r] = a.c2 * tanh_of(a.c1 * x[r]);
-        } else {
+            for (int r = 0; r < 16; r++) y[r] = log2_bias(a, h, kb + 4 * half + reg_row(r) - pos);
 #pragma unroll
-            for (int r = 0; r < 16; r++) x[r] *= a.c1;
-        }
-        if (a.table) {
-            // distances of the block, over its queries
-            const int lo = kb - (i_last + s.shift), hi = kb + 31 - (i_first + s.shift);
-            if (hi <= -a.reach || lo >= a.reach) {
-                const float c = hi <= -a.reach ? far_left : far_right;
-#pragma unroll
-                for (int r = 0; r < 16; r++) x[r] += c;
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; r++)
-                    x[r] += log2_bias(a, h, kb + 4 * half + reg_row(r) - pos);
-            }
+            for (int r = 0; r < 16; r++) x[r] += y[r];
         }
         if (kb + 32 > seen_first || kb + 32 > end) {
             const int left = lim - kb - 4 * half;
@@ -354,23 +340,20 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
         }
         float top = x[0];
 #pragma unroll
-        for (int r = 1; r < 16; r++) top = fmaxf(top, x[r]);
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        if (__any(top > m + 8.0f)) {
-            const float nm = fmaxf(m, top);
-            const float keep = nm == -INFINITY ? 1.0f : exp2_fast(m - nm);
-            m = nm;
-            sum *= keep;
+        for (int r = 0; r < 16; r += 2) top = max3(top, x[r], x[r + 1]);
+        float d, keep;
+        if (sm.moves(top, d, keep)) {
 #pragma unroll
             for (int db = 0; db < DB; db++)
 #pragma unroll
                 for (int r = 0; r < 16; r++) acc[db][r] *= keep;
+#pragma unroll
+            for (int r = 0; r < 16; r++) x[r] -= d;
         }
-        const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
         for (int r = 0; r < 16; r++) {
-            x[r] = exp2_fast(x[r] - base);
-            sum += x[r];
+            x[r] = exp2_fast(x[r]);
+            sm.sum += x[r];
         }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -378,17 +361,18 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
             V8<T> p;
             pack(x, u, p);
 #pragma unroll
-            for (int db = 0; db < DB; db++) acc[db] = mma(Tl::cols(vt, 16 * u, db), p, acc[db]);
+            for (int db = 0; db < DB; db++) acc[db] = mma(Tl::cols(vt, ln, 16 * u, db), p, acc[db]);
         }
         __builtin_amdgcn_wave_barrier();
     }
-    sum += __shfl_xor(sum, 32, kWave);
+    sm.finish();
+    __syncthreads();  // the tiles become the buffers of the sums
 
     // the wavefronts' parts, added in order: half of the row at a time goes
     // through LDS
     if (half == 0) {
-        stat[wave][0][l] = m;
-        stat[wave][1][l] = sum;
+        stat[wave][0][l] = sm.ref;
+        stat[wave][1][l] = sm.sum;
     }
     __syncthreads();
     const int bad = first_bad;
@@ -401,9 +385,9 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < NW; w++) top = fmaxf(top, stat[w][0][l & 31]);
-    const float mine = m == -INFINITY ? (sum == 0.0f ? 0.0f : sum) : exp2_fast(m - top);
+    const float mine = split_weight(sm.ref, sm.sum, top);
     constexpr int HD = DH / 2;  // elements at a time
-    float *buf = reinterpret_cast<float *>(lds);  // [NW][32][HD], 32*HD*4 = 32*DH*2 bytes each
+    float *sums = reinterpret_cast<float *>(lds);  // [NW][32][HD]
 #pragma unroll
     for (int p = 0; p < 2; p++) {
         if (p) __syncthreads();
@@ -414,7 +398,7 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
                 float y[4];
 #pragma unroll
                 for (int c = 0; c < 4; c++) y[c] = acc[(e + c) / 16][(e + c) % 16] * mine;
-                store4(buf + (wave * 32 + (l & 31)) * HD + 8 * r4 + 4 * half, y);
+                store4(sums + (wave * 32 + (l & 31)) * HD + 8 * r4 + 4 * half, y);
             }
         }
         __syncthreads();
@@ -429,7 +413,7 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
             for (int w = 0; w < NW; w++) {
                 const float mw = stat[w][0][r], lw = stat[w][1][r];
                 total += mw == -INFINITY ? lw : lw * exp2_fast(mw - big);
-                y += *reinterpret_cast<const f32x4 *>(buf + (w * 32 + r) * HD + (c % (HD / 4)) * 4);
+                y += *reinterpret_cast<const f32x4 *>(sums + (w * 32 + r) * HD + (c % (HD / 4)) * 4);
             }
             const int gr = rt * 32 + r, qi = gr / a.group, qh = kvh * a.group + gr % a.group;
             const int64_t tok = s.q0 + qi, row = tok * a.heads + qh;
@@ -454,15 +438,12 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
     }
 }
 
-constexpr int kJoinWaves = 8;
-
-// Adds the splits of one row, where it has more than one: a workgroup per
-// (query, head), whose wavefronts take splits in turn.
+// Adds the splits of one row, where it has more than one: a wavefront per
+// (query, head).
 template <class T, bool PAGED>
-__global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(Args a, Source src, Output<T> o,
+__global__ __launch_bounds__(kWave) void k_attn_join(Args a, Source src, Output<T> o,
                                                                Split sp) {
-    __shared__ float part[kJoinWaves][kMaxHeadDim + 2];
-    const int nw = blockDim.x >> 6, wave = threadIdx.x >> 6, l = threadIdx.x & 63;
+    const int l = threadIdx.x;
     const int64_t row = blockIdx.x, t = row / a.heads, rows = a.total_q * a.heads;
     const int h = int(row - t * a.heads);
     const int b = last_at_most(a.num_seqs, t, [&](int n) { return int64_t(a.q_off[n]); });
@@ -476,30 +457,76 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(Args a, Source sr
     for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, kWave));
     float x = 0.0f, y = 0.0f, total = 0.0f;
 #pragma unroll 4
-    for (int k = wave; k < n; k += nw) {
+    for (int k = 0; k < n; k++) {
         const int64_t at = k * rows + row;
         const float m = sp.ml[2 * at], sum = sp.ml[2 * at + 1];
-        const float f = m == -INFINITY ? (sum == 0.0f ? 0.0f : sum) : exp2_fast(m - top);
+        const float f = split_weight(m, sum, top);
         total += m == -INFINITY ? sum : sum * f;
         const float *p = sp.o + at * a.dim;
         if (l < a.dim) x += p[l] * f;
         if (l + 64 < a.dim) y += p[l + 64] * f;
-    }
-    part[wave][l] = x;
-    part[wave][l + 64] = y;
-    if (l == 0) part[wave][kMaxHeadDim] = total;
-    __syncthreads();
-    if (wave > 0) return;
-    for (int w = 1; w < nw; w++) {
-        x += part[w][l];
-        y += part[w][l + 64];
-        total += part[w][kMaxHeadDim];
     }
     const float inv = inverse(total);
     const Row2 r{x * inv, y * inv};
     store_row(static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride, r,
               a.dim);
     if (o.lse && l == 0) o.lse[h * a.total_q + t] = log_sum(top, total);
+}
+
+constexpr int kManySplits = 2048;
+
+// The same for many splits (up to kManySplits) of few rows: a workgroup per
+// (query, head) and 32 elements; groups of 8 lanes take splits in turn.
+template <class T, bool PAGED>
+__global__ __launch_bounds__(kBlock) void k_attn_join_many(Args a, Source src, Output<T> o,
+                                                           Split sp) {
+    __shared__ float weight[kManySplits];
+    __shared__ float red[4][2];
+    __shared__ f32x4 part[32][8];
+    const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x, t = row / a.heads, rows = a.total_q * a.heads;
+    const int h = int(row - t * a.heads);
+    const int b = last_at_most(a.num_seqs, t, [&](int n) { return int64_t(a.q_off[n]); });
+    const Seq s = seq_at<PAGED>(a, src, b);
+    const int lim = limit(a, s, int(t - s.q0));
+    if (lim <= sp.chunk) return;
+    const int n = (lim + sp.chunk - 1) / sp.chunk;
+    float top = -INFINITY;
+    for (int k = tid; k < n; k += kBlock) {
+        weight[k] = sp.ml[2 * (k * rows + row)];
+        top = fmaxf(top, weight[k]);
+    }
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, kWave));
+    if (l == 0) red[wave][0] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
+    float total = 0.0f;
+    for (int k = tid; k < n; k += kBlock) {
+        const float m = weight[k], sum = sp.ml[2 * (k * rows + row) + 1];
+        weight[k] = split_weight(m, sum, top);
+        total += m == -INFINITY ? sum : sum * weight[k];
+    }
+    total = wave_sum(total);
+    if (l == 0) red[wave][1] = total;
+    __syncthreads();
+    total = (red[0][1] + red[1][1]) + (red[2][1] + red[3][1]);
+    const int d = blockIdx.y * 32 + (tid & 7) * 4;
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (d < a.dim) {
+#pragma unroll 4
+        for (int k = tid >> 3; k < n; k += 32)
+            x += *reinterpret_cast<const f32x4 *>(sp.o + (k * rows + row) * a.dim + d) * weight[k];
+    }
+    part[tid >> 3][tid & 7] = x;
+    __syncthreads();
+    if (tid >= 8 || d >= a.dim) return;
+    x = part[0][tid];
+    for (int k = 1; k < 32; k++) x += part[k][tid];
+    const float inv = inverse(total);
+    const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+    store4(static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride + d, y);
+    if (o.lse && d == 0) o.lse[h * a.total_q + t] = log_sum(top, total);
 }
 
 // --- launches ------------------------------------------------------------------
@@ -524,10 +551,12 @@ Plan plan_of(const tc_attn &a) {
     p.blocks = p.few ? int64_t(a.num_seqs) * a.num_kv_heads * p.row_tiles
                      : tile_slots(a.total_q, a.num_seqs, 32 * p.waves) * a.num_heads;
     p.splits = 1;
-    const int64_t want = int64_t(device_cus()) * (p.few ? 8 : 4);
+    const int64_t want = int64_t(device_cus()) * 16;
     if (p.blocks > 0 && p.blocks < want && a.max_k > 512) {
-        int64_t chunk = 256;
-        while (p.blocks * ((a.max_k + chunk - 1) / chunk) > want) chunk *= 2;
+        int64_t chunk = p.few ? 512 : 256;
+        while (p.blocks * ((a.max_k + chunk - 1) / chunk) > want ||
+               (a.max_k + chunk - 1) / chunk > kManySplits)
+            chunk *= 2;
         const int64_t n = (a.max_k + chunk - 1) / chunk;
         if (n > 1) {
             p.chunk = int(chunk);
@@ -546,28 +575,40 @@ size_t split_bytes(const tc_attn &a, const Plan &p, size_t *ml_at) {
     return *ml_at + up256(rows * 2 * sizeof(float));
 }
 
+template <class T, class CT, bool PAGED, bool CAP, int DH>
+void launch_tile(const Args &a, const Plan &p, const Source &src, tc_rows q, const Output<T> &o,
+                 const Split &sp, hipStream_t stream) {
+    constexpr int BN = tile_keys<T>(DH);
+    const dim3 grid(unsigned(p.blocks), p.splits);
+    const size_t bias = a.table ? bias_entries(a.reach) * sizeof(float) : 0;
+    const int slots = int(p.blocks / a.heads);
+    if (p.waves == 1)
+        hipLaunchKernelGGL((k_attn_tile<T, CT, PAGED, CAP, DH, 1, 32, 1>), grid, dim3(64),
+                           2 * 32 * DH * sizeof(T) + bias, stream, a, src, q, o, sp, slots);
+    else
+        hipLaunchKernelGGL((k_attn_tile<T, CT, PAGED, CAP, DH, 4, BN, 2>), grid, dim3(256),
+                           4 * BN * DH * sizeof(T) + bias, stream, a, src, q, o, sp, slots);
+}
+
 template <class T, class CT, bool PAGED, int DH>
 void launch(const tc_attn &t, const Args &a, const Plan &p, const Source &src, tc_rows q,
             const Output<T> &o, const Split &sp, hipStream_t stream) {
-    constexpr int BN = sizeof(T) == 4 ? 32 : 64;
-    const dim3 grid(unsigned(p.blocks), p.splits);
-    if (p.few) {
-        hipLaunchKernelGGL((k_attn_few<T, CT, PAGED, DH>), grid, dim3(kBlock),
-                           4 * 32 * DH * sizeof(T), stream, a, src, q, o, sp, p.row_tiles);
-    } else {
-        const size_t bias = a.table ? bias_entries(a.reach) * sizeof(float) : 0;
-        const int slots = int(p.blocks / a.heads);
-        if (p.waves == 1)
-            hipLaunchKernelGGL((k_attn_tile<T, CT, PAGED, DH, 1, 32>), grid, dim3(64),
-                               2 * 32 * DH * sizeof(T) + bias, stream, a, src, q, o, sp, slots);
-        else
-            hipLaunchKernelGGL((k_attn_tile<T, CT, PAGED, DH, 4, BN>), grid, dim3(256),
-                               2 * BN * DH * sizeof(T) + bias, stream, a, src, q, o, sp, slots);
-    }
+    if (p.few)
+        hipLaunchKernelGGL((k_attn_few<T, CT, PAGED, DH>), dim3(unsigned(p.blocks), p.splits),
+                           dim3(kBlock), 4 * 2 * 32 * DH * sizeof(T), stream, a, src, q, o, sp,
+                           p.row_tiles);
+    else if (a.capped)
+        launch_tile<T, CT, PAGED, true, DH>(a, p, src, q, o, sp, stream);
+    else
+        launch_tile<T, CT, PAGED, false, DH>(a, p, src, q, o, sp, stream);
     if (p.splits > 1) {
-        const int nw = p.splits >= 16 ? kJoinWaves : 1;
-        hipLaunchKernelGGL((k_attn_join<T, PAGED>), dim3(unsigned(t.total_q * t.num_heads)),
-                           dim3(nw * 64), 0, stream, a, src, o, sp);
+        const unsigned rows = unsigned(t.total_q * t.num_heads);
+        if (p.splits >= 16)
+            hipLaunchKernelGGL((k_attn_join_many<T, PAGED>), dim3(rows, (a.dim + 31) / 32),
+                               dim3(kBlock), 0, stream, a, src, o, sp);
+        else
+            hipLaunchKernelGGL((k_attn_join<T, PAGED>), dim3(rows), dim3(kWave), 0, stream, a, src,
+                               o, sp);
     }
 }
 

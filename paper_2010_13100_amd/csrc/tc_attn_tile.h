@@ -20,6 +20,8 @@
 // reads of 32 columns from 8 rows spread over the banks.
 #pragma once
 
+#include <type_traits>
+
 #include "tc_attn.h"
 
 namespace tc {
@@ -90,19 +92,12 @@ __device__ __forceinline__ Raw<bf16> load_raw(const bf16 *p, uint32_t) {
 __device__ __forceinline__ Raw<fp8> load_raw(const fp8 *p, uint32_t e) {
     return {*reinterpret_cast<const u32x2 *>(p), e};
 }
-template <class CT>
-__device__ __forceinline__ Raw<CT> zero_raw();
-template <>
-__device__ __forceinline__ Raw<float> zero_raw<float>() {
-    return {f32x8{0, 0, 0, 0, 0, 0, 0, 0}};
-}
-template <>
-__device__ __forceinline__ Raw<bf16> zero_raw<bf16>() {
-    return {__builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0})};
-}
-template <>
-__device__ __forceinline__ Raw<fp8> zero_raw<fp8>() {
-    return {u32x2{0, 0}, 127};
+template <class T>
+__device__ __forceinline__ V8<T> zero8() {
+    V8<T> x;
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = T(0.0f);
+    return x;
 }
 
 // As elements of the products. 8-bit values times a power of two are exact.
@@ -171,45 +166,244 @@ struct Tile {
     static __device__ __forceinline__ void put(T *t, int row, int chunk, const V8<T> &x) {
         *reinterpret_cast<V8<T> *>(t + at(row, chunk)) = x;
     }
-    // Left operand: rows r0 .. r0+31, values 16*ks .. +15 of each.
-    static __device__ __forceinline__ V8<T> rows(const T *t, int r0, int ks) {
-        const int l = threadIdx.x & 63;
-        return *reinterpret_cast<const V8<T> *>(t + at(r0 + (l & 31), 2 * ks + (l >> 5)));
+    // What a lane adds to a tile's start for its operands; everything else of
+    // their addresses is known to the compiler (chunks 8 apart and rows 8 apart
+    // have the same places).
+    struct Lane {
+        int row[4];                        // chunks 2*ks + half, ks = 0 .. 3
+        int col[sizeof(T) == 2 ? 2 : 8];   // column blocks 0 and 1
+    };
+    static __device__ __forceinline__ Lane lane() {
+        const int l = threadIdx.x & 63, half = l >> 5;
+        Lane a;
+#pragma unroll
+        for (int ks = 0; ks < 4; ks++) a.row[ks] = at(l & 31, 2 * ks + half);
+        if constexpr (sizeof(T) == 2) {
+            // 16 lanes read a 4 x 16 block of 16-bit values transposed: lane j
+            // gives the address of row j/4, values 4*(j%4) .. +3, and gets column j
+            const int j = l & 15, d = ((l >> 4) & 1) * 16 + (j & 3) * 4;
+#pragma unroll
+            for (int db = 0; db < 2; db++)
+                a.col[db] = at(4 * half + (j >> 2), 4 * db + (d >> 3)) + (d & 7);
+        } else {
+#pragma unroll
+            for (int n = 0; n < 8; n++)
+                a.col[n] = at(4 * half + (n & 3), 4 * (n >> 2) + ((l & 31) >> 3)) + (l & 7);
+        }
+        return a;
+    }
+    // Left operand: rows r0 .. r0+31 (r0 a multiple of 8), values 16*ks .. +15 of
+    // each.
+    static __device__ __forceinline__ V8<T> rows(const T *t, const Lane &a, int r0, int ks) {
+        return *reinterpret_cast<const V8<T> *>(t + a.row[ks & 3] + r0 * DH + (ks >> 2) * 64);
     }
     // Left operand of the transposed tile: columns 32*db .. +31 as rows; its 16
     // values are the tile's rows r0 .. r0+15 in the order of a block's
     // registers. r0 is a multiple of 16.
-    static __device__ __forceinline__ V8<T> cols(const T *t, int r0, int db) {
-        const int l = threadIdx.x & 63, half = l >> 5;
+    static __device__ __forceinline__ V8<T> cols(const T *t, const Lane &a, int r0, int db) {
         V8<T> x;
         if constexpr (sizeof(T) == 2) {
-            // 16 lanes read a 4 x 16 block of 16-bit values transposed: lane j
-            // gives the address of row j/4, values 4*(j%4) .. +3, and gets column j
-            const int j = l & 15, row = 4 * half + (j >> 2);
-            const int d = db * 32 + ((l >> 4) & 1) * 16 + (j & 3) * 4;
-            const T *p = t + r0 * DH + at(row, d >> 3) + (d & 7);
+            const T *p = t + a.col[db & 1] + r0 * DH + (db >> 1) * 64;
             typedef __attribute__((address_space(3))) s16x4 lds4;
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p));
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 8 * DH));
-            x = __builtin_bit_cast(V8<T>, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+            const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p));
+            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 8 * DH));
+            x = __builtin_bit_cast(V8<T>, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const int d = db * 32 + (l & 31);
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const int row = 4 * half + (i < 4 ? i : i + 4);
-                x[i] = t[r0 * DH + at(row, d >> 3) + (d & 7)];
-            }
+            for (int i = 0; i < 8; i++)
+                x[i] = t[a.col[(db & 1) * 4 + (i & 3)] + (r0 + (i < 4 ? 0 : 8)) * DH + (db >> 1) * 64];
         }
         return x;
     }
 };
 
+// --- from memory to LDS ---------------------------------------------------------
+//
+// A thread loads its share of a tile into registers while the tile before is
+// worked on, and puts it into LDS afterwards. (Loads that go to LDS by
+// themselves were slower: 1035 us against 870 for 2 x 8192 causal queries and
+// 16 heads of 128 bf16.) Loads are straight-line code: a load under a
+// condition makes the compiler wait for the ones before it. Rows past the end
+// repeat the last one (they get weight 0), elements past head_dim the first
+// ones (and become 0 in LDS).
+
+// Keeps what is under a uniform condition under a branch: the compiler would
+// otherwise select between its results in every lane.
+__device__ __forceinline__ void apart() { asm volatile(""); }
+
+// The largest of three, without the passes over each operand that make a
+// signalling NaN quiet (none arises here).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
+
+// NT threads load ROWS rows of two arrays.
+template <class T, class CT, int DH, int NT, int ROWS>
+struct Stage {
+    typedef Tile<T, DH> Tl;
+    static constexpr bool Q8 = sizeof(CT) == 1;
+    static constexpr int EL = Q8 ? 16 : 8;                                // elements of a load
+    static constexpr int LPR = DH / EL;                                   // lanes of a row
+    static constexpr int IT = ROWS * LPR >= NT ? ROWS * LPR / NT : 1;     // rows of a lane
+    static constexpr int STEP = NT / LPR;                                 // rows between them
+    static_assert(NT % LPR == 0 && (ROWS * LPR % NT == 0 || ROWS * LPR < NT), "");
+
+    struct Data {
+        typename std::conditional<Q8, u32x4, Raw<CT>>::type x;
+    };
+    int tid, row0, elem;
+    bool live, half_live;  // this lane's elements (8 bits: the second 8) are in the row
+    bool pad;              // some lane's are not
+    uint32_t ko, vo;       // dense: byte offsets of row 0 of the lane
+    int page[IT];
+    Data a[IT], b[IT];
+    uint32_t ae[Q8 ? IT : 1], be[Q8 ? IT : 1];
+
+    __device__ __forceinline__ void init(int t, int dim) {
+        tid = t;
+        row0 = t / LPR;
+        const int e = (t % LPR) * EL;
+        live = e < dim;
+        half_live = e + 8 < dim;
+        pad = dim < DH;
+        elem = live ? e : 0;
+    }
+    static __device__ __forceinline__ void get(Data &d, const float *p, bool) { d.x = load_raw(p, 0); }
+    static __device__ __forceinline__ void get(Data &d, const bf16 *p, bool) { d.x = load_raw(p, 0); }
+    static __device__ __forceinline__ void get(Data &d, const fp8 *p, bool both) {
+        // rows start at multiples of 8 bytes and may end after 8 of the 16
+        typedef u32x4 u32x4_8 __attribute__((aligned(8)));
+        if (both) {  // (uniform)
+            d.x = *reinterpret_cast<const u32x4_8 *>(p);
+        } else {
+            const u32x2 y = *reinterpret_cast<const u32x2 *>(p);
+            d.x = u32x4{y[0], y[1], 0, 0};
+        }
+    }
+    // Rows base + r*stride of two arrays, r from first to last at most.
+    __device__ __forceinline__ void load_rows(const CT *ap, const CT *bp, int64_t as, int64_t bs,
+                                              int first, int last) {
+        const CT *au = ap + first * as, *bu = bp + first * bs;  // (uniform)
+        if (first + ROWS - 1 <= last) {
+#pragma unroll
+            for (int n = 0; n < IT; n++) {
+                const uint32_t r = (ROWS * LPR < NT) ? min(row0, ROWS - 1) : row0;
+                get(a[n], au + n * STEP * as + (r * uint32_t(as) + elem), true);
+                get(b[n], bu + n * STEP * bs + (r * uint32_t(bs) + elem), true);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < IT; n++) {
+                const uint32_t r = min(row0 + n * STEP, last - first);
+                get(a[n], au + (r * uint32_t(as) + elem), true);
+                get(b[n], bu + (r * uint32_t(bs) + elem), true);
+            }
+        }
+    }
+    // The pages of the tile from key kb on.
+    template <class KV>
+    __device__ __forceinline__ void look_up(const KV &kv, int kb, int end) {
+        if constexpr (KV::paged) {
+            if (kb < end) {
+#pragma unroll
+                for (int n = 0; n < IT; n++) page[n] = kv.page(min(kb + row0 + n * STEP, end - 1));
+            }
+        }
+    }
+    // Starts the loads of keys kb .. (below end); pages have been looked up.
+    template <class KV>
+    __device__ __forceinline__ void load(const KV &kv, int kb, int end, int dim) {
+        if constexpr (KV::paged) {
+            const bool both = (dim & 8) == 0;
+            Loc at[IT];
+#pragma unroll
+            for (int n = 0; n < IT; n++) at[n] = kv.loc(min(kb + row0 + n * STEP, end - 1), page[n]);
+            if constexpr (Q8) {
+#pragma unroll
+                for (int n = 0; n < IT; n++) {
+                    ae[n] = kv.k_exp(at[n]);
+                    be[n] = kv.v_exp(at[n]);
+                }
+            }
+            if (both || !Q8) {
+#pragma unroll
+                for (int n = 0; n < IT; n++) {
+                    get(a[n], kv.k(at[n]) + elem, true);
+                    get(b[n], kv.v(at[n]) + elem, true);
+                }
+            } else if constexpr (Q8) {
+#pragma unroll
+                for (int n = 0; n < IT; n++) {
+                    Data x, y;
+                    get(a[n], kv.k(at[n]) + elem, false);
+                    get(x, kv.k(at[n]) + (half_live ? elem + 8 : 0), false);
+                    get(b[n], kv.v(at[n]) + elem, false);
+                    get(y, kv.v(at[n]) + (half_live ? elem + 8 : 0), false);
+                    a[n].x[2] = x.x[0], a[n].x[3] = x.x[1];
+                    b[n].x[2] = y.x[0], b[n].x[3] = y.x[1];
+                }
+            }
+        } else {
+            load_rows(kv.kp, kv.vp, kv.kts, kv.vts, kb, end - 1);
+        }
+    }
+    __device__ __forceinline__ void put_one(T *t, int row, const Data &d, uint32_t e) {
+        if constexpr (Q8) {
+            V8<T> x, y;
+            expand(Raw<fp8>{u32x2{d.x[0], d.x[1]}, e}, x);
+            expand(Raw<fp8>{u32x2{d.x[2], d.x[3]}, e}, y);
+            if (pad) {
+                apart();
+                x = live ? x : zero8<T>();
+                y = half_live ? y : zero8<T>();
+            }
+            Tl::put(t, row, 2 * (tid % LPR), x);
+            Tl::put(t, row, 2 * (tid % LPR) + 1, y);
+        } else {
+            V8<T> x;
+            expand(d.x, x);
+            if (pad) {
+                apart();
+                x = live ? x : zero8<T>();
+            }
+            Tl::put(t, row, tid % LPR, x);
+        }
+    }
+    __device__ __forceinline__ void put(T *at, T *bt) {
+#pragma unroll
+        for (int n = 0; n < IT; n++) {
+            const int row = row0 + n * STEP;
+            if (ROWS * LPR < NT && row >= ROWS) return;
+            put_one(at, row, a[n], ae[Q8 ? n : 0]);
+            put_one(bt, row, b[n], be[Q8 ? n : 0]);
+        }
+    }
+};
+
+// Sets what is not finite in this thread's part of a tile of ROWS rows to zero
+// and calls each(row) for every such row. Between two barriers.
+template <class T, int DH, int NT, int ROWS, class Each>
+__device__ __forceinline__ void clean_tile(T *t, int tid, Each each) {
+    constexpr int CPR = DH / 8;
+#pragma unroll 1
+    for (int r = tid / CPR; r < ROWS; r += NT / CPR) {
+        V8<T> *p = reinterpret_cast<V8<T> *>(t + r * DH + (tid % CPR) * 8);
+        V8<T> x = *p;
+        if (clean(x)) {
+            *p = x;
+            each(r);
+        }
+    }
+}
+
 // Right operand from a row in memory: columns are rows of 8-element chunks.
 template <class T>
 __device__ __forceinline__ V8<T> chunk_of(const T *row, int chunk, int dim) {
     V8<T> x;
-    expand(chunk * 8 < dim ? load_raw(row + chunk * 8, 0) : zero_raw<T>(), x);
-    return x;
+    expand(load_raw(row + (chunk * 8 < dim ? chunk * 8 : 0), 0), x);
+    return chunk * 8 < dim ? x : zero8<T>();
 }
 
 // Writes a transposed block (rows are elements 32*db .. +31 of this lane's
@@ -274,42 +468,110 @@ __device__ __forceinline__ int seq_of_slot(const int32_t *off, int num_seqs, int
 constexpr int kBiasPad = 63;
 inline int bias_entries(int reach) { return 2 * (reach + kBiasPad) + 1; }
 
-__device__ __forceinline__ void load_bias(const Args &a, int h, float *lds) {
-    const int n = 2 * (a.reach + kBiasPad) + 1;
-    for (int i = threadIdx.x; i < n; i += blockDim.x)
+// Loads the entries of distances lo to hi and the two ends.
+__device__ __forceinline__ void load_bias(const Args &a, int h, int lo, int hi, float *lds) {
+    const int last = 2 * (a.reach + kBiasPad);
+    const int from = max(lo + a.reach + kBiasPad, 0), to = min(hi + a.reach + kBiasPad, last);
+#pragma unroll 4
+    for (int i = from + int(threadIdx.x); i <= to; i += blockDim.x)
         lds[i] = log2_bias(a, h, i - a.reach - kBiasPad);
+    if (threadIdx.x < 2) {
+        const int i = threadIdx.x ? last : 0;
+        lds[i] = log2_bias(a, h, i - a.reach - kBiasPad);
+    }
 }
 
-// Adds the bias to a block of scores whose distance at (row 0, column 0) is
-// `rel`: this lane's registers are keys 4*half + reg_row(r), query col.
+// Whether a block with distance `rel` at row 0, column 0 lies within the reach
+// somewhere; if not, all its entries have the bias far_bias (uniform).
+__device__ __forceinline__ bool near_block(const Args &a, int rel) {
+    return rel + 31 > -a.reach && rel - 31 < a.reach;
+}
+__device__ __forceinline__ float far_bias(const Args &a, const float *lds, int rel) {
+    return lds[rel < 0 ? 0 : 2 * (a.reach + kBiasPad)];
+}
+// Adds the bias to such a block whose rows are keys, 4*half + reg_row(r) in this
+// lane, and columns queries.
 __device__ __forceinline__ void add_bias(const Args &a, const float *lds, int rel, f32x16 &x) {
     const int l = threadIdx.x & 63;
-    if (rel + 31 <= -a.reach || rel - 31 >= a.reach) {
-        const float c = lds[rel < 0 ? 0 : 2 * (a.reach + kBiasPad)];
-#pragma unroll
-        for (int r = 0; r < 16; r++) x[r] += c;
-        return;
-    }
     const float *p = lds + (rel + 4 * (l >> 5) - (l & 31) + a.reach + kBiasPad);
 #pragma unroll
     for (int r = 0; r < 16; r++) x[r] += p[reg_row(r)];
 }
-
-// The same for a block whose rows are queries: this lane's registers are
-// queries 4*half + reg_row(r), key col.
+// The same where rows are queries and columns keys.
 __device__ __forceinline__ void add_bias_queries(const Args &a, const float *lds, int rel,
                                                  f32x16 &x) {
     const int l = threadIdx.x & 63;
-    if (rel + 31 <= -a.reach || rel - 31 >= a.reach) {
-        const float c = lds[rel < 0 ? 0 : 2 * (a.reach + kBiasPad)];
-#pragma unroll
-        for (int r = 0; r < 16; r++) x[r] += c;
-        return;
-    }
     const float *p = lds + (rel - 4 * (l >> 5) + (l & 31) + a.reach + kBiasPad);
 #pragma unroll
     for (int r = 0; r < 16; r++) x[r] += p[-reg_row(r)];
 }
+
+// Products to scores, plus c0.
+template <bool CAP>
+__device__ __forceinline__ void to_scores(const Args &a, float c0, f32x16 &x) {
+    if (CAP) {
+        const float f = -2.0f * a.c2, k = a.c2 + c0;
+#pragma unroll
+        for (int r = 0; r < 16; r++) x[r] = __builtin_fmaf(f, half_tanh(a.c1 * x[r]), k);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; r++) x[r] = __builtin_fmaf(x[r], a.c1, c0);
+    }
+}
+// The same, and the scores' derivative by the product over deriv_scale() (0
+// without a cap, where it is 1 and not used).
+struct Scores {
+    f32x16 x, f;
+};
+template <bool CAP>
+__device__ __forceinline__ Scores scores_of(const Args &a, float c0, f32x16 z) {
+    Scores s;
+    if (CAP) {
+        const float g = -2.0f * a.c2, k = a.c2 + c0;
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            const float t = half_tanh(a.c1 * z[r]);
+            s.x[r] = __builtin_fmaf(g, t, k);
+            s.f[r] = __builtin_fmaf(-t, t, t);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            s.x[r] = __builtin_fmaf(z[r], a.c1, c0);
+            s.f[r] = 0.0f;
+        }
+    }
+    return s;
+}
+__device__ __forceinline__ float deriv_scale(const Args &a) {
+    return a.capped ? 4.0f * a.scale : a.scale;
+}
+
+// The running softmax of a lane's row: scores are formed minus `ref`, a value
+// near the row's maximum: the first seen, then raised when a score passes it by
+// 2^8. Within 2^8 nothing is lost in fp32 sums, and most tiles do not move it.
+struct Softmax {
+    float ref = 0.0f, sum = 0.0f;
+    bool fresh = true;  // no key seen
+    // For a block's scores minus ref with maximum `top` in this half: true if
+    // some row's ref moves; then all scores go down by d, sums are times keep.
+    __device__ __forceinline__ bool moves(float top, float &d, float &keep) {
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        if (!__any(top > 8.0f || (fresh && top > -INFINITY))) return false;
+        const bool seen = top > -INFINITY;
+        d = fresh ? (seen ? top : 0.0f) : fmaxf(top, 0.0f);
+        keep = exp2_fast(-d);
+        fresh = fresh && !seen;
+        ref += d;
+        sum *= keep;
+        return true;
+    }
+    // Maximum-like value and sum of the whole row; -inf if it saw nothing.
+    __device__ __forceinline__ void finish() {
+        sum += __shfl_xor(sum, 32, kWave);
+        if (sum == 0.0f) ref = -INFINITY;
+    }
+};
 
 }  // namespace attn
 }  // namespace tc

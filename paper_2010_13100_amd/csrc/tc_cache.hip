@@ -222,6 +222,9 @@ tc_status check_rows(const char *fn, const char *name, const tc_rows &r, int32_t
     const int64_t unit = dtype == TC_F32 ? 4 : 8;  // elements of 16 bytes
     TC_REQUIRE(r.token_stride >= 0 && r.head_stride >= 0, TC_ERR_INVALID_ARG,
                "%s: %s has a negative stride", fn, name);
+    // (a tile's rows are found by 32-bit offsets from its first)
+    TC_REQUIRE(r.token_stride < (int64_t(1) << 24), TC_ERR_UNSUPPORTED,
+               "%s: rows of %s are 2^24 elements or more apart", fn, name);
     TC_REQUIRE(aligned16(r.data) && r.token_stride % unit == 0 && r.head_stride % unit == 0,
                TC_ERR_UNSUPPORTED, "%s: rows of %s must start at multiples of 16 bytes", fn, name);
     return TC_OK;
