@@ -16,8 +16,13 @@
 // eight 32x32x2 instructions.
 //
 // A tile in LDS has rows of DH elements in chunks of 8; chunk c of row r is at
-// place c ^ (r & 7), so that reads of one chunk from 32 rows and transposed
-// reads of 32 columns from 8 rows spread over the banks.
+// place c ^ place(r). Two kinds of reads have to spread over the 256 bytes of the
+// banks: one chunk of 32 rows, and 32 columns of 4 rows, transposed. For 16-bit
+// elements the columns are 64 bytes of a row, so bits of the row that differ
+// among the 4 choose the 64-byte window of the 256 (in rows of 128 bytes the
+// row's lowest bit does so by itself) and others the chunk within it; fp32
+// columns are 128 bytes. Bit 3 of the row is never used: rows 8 apart have the
+// same places.
 #pragma once
 
 #include <type_traits>
@@ -160,42 +165,42 @@ __device__ __forceinline__ bool clean(bf16x8 &x) {
 
 template <class T, int DH>
 struct Tile {
+    static __device__ __forceinline__ int place(int row) {
+        if (sizeof(T) == 4) return row & 7;
+        if (DH == 64) return (row & 2) << 1 | (row >> 2 & 1) | (row >> 3 & 2);
+        return (row & 3) << 2 | (row >> 2 & 1) | (row >> 3 & 2);
+    }
     static __device__ __forceinline__ int at(int row, int chunk) {
-        return row * DH + ((chunk ^ (row & 7)) << 3);
+        return row * DH + ((chunk ^ place(row)) << 3);
     }
     static __device__ __forceinline__ void put(T *t, int row, int chunk, const V8<T> &x) {
         *reinterpret_cast<V8<T> *>(t + at(row, chunk)) = x;
     }
-    // What a lane adds to a tile's start for its operands; everything else of
-    // their addresses is known to the compiler (chunks 8 apart and rows 8 apart
-    // have the same places).
+    // What a lane adds to a tile's start for its operands: another chunk is an
+    // exclusive or of its bits away.
     struct Lane {
-        int row[4];                        // chunks 2*ks + half, ks = 0 .. 3
-        int col[sizeof(T) == 2 ? 2 : 8];   // column blocks 0 and 1
+        int row;                           // row l%32, chunk l/32
+        int col[sizeof(T) == 2 ? 1 : 4];   // the first columns' rows
     };
     static __device__ __forceinline__ Lane lane() {
         const int l = threadIdx.x & 63, half = l >> 5;
         Lane a;
-#pragma unroll
-        for (int ks = 0; ks < 4; ks++) a.row[ks] = at(l & 31, 2 * ks + half);
+        a.row = at(l & 31, half);
         if constexpr (sizeof(T) == 2) {
             // 16 lanes read a 4 x 16 block of 16-bit values transposed: lane j
             // gives the address of row j/4, values 4*(j%4) .. +3, and gets column j
             const int j = l & 15, d = ((l >> 4) & 1) * 16 + (j & 3) * 4;
-#pragma unroll
-            for (int db = 0; db < 2; db++)
-                a.col[db] = at(4 * half + (j >> 2), 4 * db + (d >> 3)) + (d & 7);
+            a.col[0] = at(4 * half + (j >> 2), d >> 3) + (d & 7);
         } else {
 #pragma unroll
-            for (int n = 0; n < 8; n++)
-                a.col[n] = at(4 * half + (n & 3), 4 * (n >> 2) + ((l & 31) >> 3)) + (l & 7);
+            for (int n = 0; n < 4; n++) a.col[n] = at(4 * half + n, (l & 31) >> 3) + (l & 7);
         }
         return a;
     }
-    // Left operand: rows r0 .. r0+31 (r0 a multiple of 8), values 16*ks .. +15 of
+    // Left operand: rows r0 .. r0+31 (r0 a multiple of 32), values 16*ks .. +15 of
     // each.
     static __device__ __forceinline__ V8<T> rows(const T *t, const Lane &a, int r0, int ks) {
-        return *reinterpret_cast<const V8<T> *>(t + a.row[ks & 3] + r0 * DH + (ks >> 2) * 64);
+        return *reinterpret_cast<const V8<T> *>(t + (a.row ^ (2 * ks) << 3) + r0 * DH);
     }
     // Left operand of the transposed tile: columns 32*db .. +31 as rows; its 16
     // values are the tile's rows r0 .. r0+15 in the order of a block's
@@ -203,7 +208,7 @@ struct Tile {
     static __device__ __forceinline__ V8<T> cols(const T *t, const Lane &a, int r0, int db) {
         V8<T> x;
         if constexpr (sizeof(T) == 2) {
-            const T *p = t + a.col[db & 1] + r0 * DH + (db >> 1) * 64;
+            const T *p = t + (a.col[0] ^ (4 * db ^ (r0 >> 3 & 2)) << 3) + r0 * DH;
             typedef __attribute__((address_space(3))) s16x4 lds4;
             const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p));
             const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 8 * DH));
@@ -211,7 +216,7 @@ struct Tile {
         } else {
 #pragma unroll
             for (int i = 0; i < 8; i++)
-                x[i] = t[a.col[(db & 1) * 4 + (i & 3)] + (r0 + (i < 4 ? 0 : 8)) * DH + (db >> 1) * 64];
+                x[i] = t[(a.col[i & 3] ^ (4 * db) << 3) + (r0 + (i < 4 ? 0 : 8)) * DH];
         }
         return x;
     }
