@@ -242,6 +242,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
 #pragma unroll
             for (int r = 0; r < 16; r++) x[r] = exp2_fast(x[r]) * (dp[r] - delta);
             if (k0 + 32 > lim_first) {
+                apart();
                 const int left = lim - k0 - 4 * half;
 #pragma unroll
                 for (int r = 0; r < 16; r++) x[r] = reg_row(r) < left ? x[r] : 0.0f;
@@ -291,7 +292,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
 // so that their sum needs no atomics. Blocks have queries as rows here (the
 // products that follow sum over them).
 //
-// A workgroup takes every gridDim.x-th tile of its heads and, with DIST, keeps
+// A workgroup takes every gridDim.y-th tile of its heads (all heads of a tile run
+// together, and a sequence's first tiles, which most queries see, first) and, with DIST, keeps
 // one sum per head, distance and wavefront in LDS throughout, so that the order
 // of the terms is fixed. Where those of all its heads do not fit (kept = 1) it
 // keeps one head's and adds them to its own row in the workspace after each.
@@ -312,7 +314,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     T *values = tiles + NBUF * 2 * BQ * DH;
     float *bias = reinterpret_cast<float *>(values + (VLDS ? BM * DH : 0));
     const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, half = l >> 5;
-    const int h0 = blockIdx.y * span, kvh = h0 / a.group, width = 2 * a.reach + 1;
+    const int h0 = blockIdx.x * span, kvh = h0 / a.group, width = 2 * a.reach + 1;
     float *skew = bias + (a.table ? 2 * (a.reach + kBiasPad) + 1 : 0) + wave * kSkewFloats;
     float *dists = skew + (NW - wave) * kSkewFloats;  // [kept][NW][width]
     float far_left = 0.0f, far_right = 0.0f;
@@ -322,7 +324,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     // to what the row holds
     auto flush = [&](int h, int at, bool add) {
         __syncthreads();
-        float *p = g.bias_part + (int64_t(h) * gridDim.x + blockIdx.x) * width;
+        float *p = g.bias_part + (int64_t(h) * gridDim.y + blockIdx.y) * width;
         for (int d = threadIdx.x; d < width; d += NT) {
             float x = dists[at + d];
 #pragma unroll
@@ -334,7 +336,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     Stage<T, T, DH, NT, BQ> st;
     st.init(tid, a.dim);
 
-    for (int slot = blockIdx.x; slot < slots; slot += int(gridDim.x)) {
+    for (int slot = blockIdx.y; slot < slots; slot += int(gridDim.y)) {
     int tile;
     const int b = seq_of_slot(a.k_off, a.num_seqs, slot, BM, tile);
     const Seq s = seq_of(a, b, -1);
@@ -371,14 +373,13 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     for (int db = 0; db < DB; db++) dk[db] = dv[db] = zero16();
 
     float lse_r = 0.0f, delta_r = 0.0f;
-    auto fetch = [&](int h, int qb) {
-        st.load_rows(static_cast<const T *>(g.q.data) + s.q0 * g.q.token_stride + h * g.q.head_stride,
-                     static_cast<const T *>(g.grad_out.data) + s.q0 * g.grad_out.token_stride +
-                         h * g.grad_out.head_stride,
-                     g.q.token_stride, g.grad_out.token_stride, qb, s.qn - 1);
-        const int64_t t = h * a.total_q + s.q0 + min(qb + (tid & (BQ - 1)), s.qn - 1);
-        lse_r = g.lse[t] * kLog2e;
-        delta_r = g.delta[t];
+    const T *qrow, *orow;  // of the head, with what follows
+    const float *lse, *delta;
+    auto fetch = [&](int qb) {
+        st.load_rows(qrow, orow, g.q.token_stride, g.grad_out.token_stride, qb, s.qn - 1);
+        const int i = min(qb + (tid & (BQ - 1)), s.qn - 1);
+        lse_r = lse[i] * kLog2e;
+        delta_r = delta[i];
     };
     auto put = [&](int n) {
         T *p = tiles + n * 2 * BQ * DH;
@@ -391,7 +392,12 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     for (int hg = 0; hg < span; hg++) {
         const int h = h0 + hg;
         float *dist = dists + ((kept > 1 ? hg : 0) * NW + wave) * width;
-        if (begin < s.qn) fetch(h, begin);
+        qrow = static_cast<const T *>(g.q.data) + s.q0 * g.q.token_stride + h * g.q.head_stride;
+        orow = static_cast<const T *>(g.grad_out.data) + s.q0 * g.grad_out.token_stride +
+               h * g.grad_out.head_stride;
+        lse = g.lse + h * a.total_q + s.q0;
+        delta = g.delta + h * a.total_q + s.q0;
+        if (begin < s.qn) fetch(begin);
         __syncthreads();  // the last head's tiles and bias have been read
         if (a.table) load_bias(a, h, j0 - (s.qn - 1 + s.shift), j0 + BM - 1 - (begin + s.shift), bias);
         if (begin < s.qn) put(0);
@@ -406,7 +412,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
                 __syncthreads();
             }
             const bool more = qb + BQ < s.qn;
-            if (NBUF == 2 && more) fetch(h, qb + BQ);
+            if (NBUF == 2 && more) fetch(qb + BQ);
             const int now = buf;
 #pragma unroll
             for (int n = 0; n < BQ / 32; n++) {
@@ -426,18 +432,19 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
                 if (near) add_bias_queries(a, bias, rel, x);
 #pragma unroll
                 for (int c = 0; c < 4; c++) {
-                    const f32x4 lse = *reinterpret_cast<const f32x4 *>(
+                    const f32x4 sum = *reinterpret_cast<const f32x4 *>(
                         &stat[now][0][32 * n + 8 * c + 4 * half]);
                     const f32x4 del = *reinterpret_cast<const f32x4 *>(
                         &stat[now][1][32 * n + 8 * c + 4 * half]);
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
                         const int r = 4 * c + e;
-                        x[r] = exp2_fast(x[r] - lse[e]);
+                        x[r] = exp2_fast(x[r] - sum[e]);
                         dp[r] = x[r] * (dp[r] - del[e]);
                     }
                 }
                 if (q0 < fq_last || q0 + 32 > s.qn) {  // queries that see the key, up to the last
+                    apart();
                     const int from = fq - q0 - 4 * half, to = s.qn - q0 - 4 * half;
 #pragma unroll
                     for (int r = 0; r < 16; r++) {
@@ -448,6 +455,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
                 }
                 if (DIST) {
                     if (w0 + 32 > s.kn) {  // keys past the last one repeat it
+                        apart();
 #pragma unroll
                         for (int r = 0; r < 16; r++) dp[r] = j < s.kn ? dp[r] : 0.0f;
                     }
@@ -470,7 +478,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
                 }
             }
             if (NBUF == 1) {
-                if (more) fetch(h, qb + BQ);
+                if (more) fetch(qb + BQ);
                 __syncthreads();
             } else {
                 buf ^= 1;
@@ -665,14 +673,14 @@ Space space_of(const tc_attn &a) {
 
 template <class T, bool CAP, int DH, int NW, bool DIST>
 void launch_dkv(const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
-    constexpr int NBUF = NW == 1 ? 1 : 2;
+    constexpr int NBUF = NW == 1 ? 1 : 2, BQ = NW == 1 || sizeof(T) * DH > 256 ? 32 : 64;
     const size_t width = DIST ? (2 * a.reach + 1) * sizeof(float) : 0;
     // sums by distance of all heads of a workgroup in 32 KB, or of one
     const int kept = size_t(p.span) * NW * width <= (32 << 10) ? p.span : 1;
-    const size_t bytes = (NBUF * 2 * 32 + (sizeof(T) * DH > 256 ? NW * 32 : 0)) * DH * sizeof(T) +
+    const size_t bytes = (NBUF * 2 * BQ + (sizeof(T) * DH > 256 ? NW * 32 : 0)) * DH * sizeof(T) +
                          (a.table ? bias_entries(a.reach) * sizeof(float) : 0) +
                          (DIST ? NW * kSkewFloats * sizeof(float) : 0) + kept * NW * width;
-    hipLaunchKernelGGL((k_attn_dkv<T, CAP, DH, NW, 32, DIST, NBUF>), dim3(p.parts, a.heads / p.span),
+    hipLaunchKernelGGL((k_attn_dkv<T, CAP, DH, NW, BQ, DIST, NBUF>), dim3(a.heads / p.span, p.parts),
                        dim3(NW * 64), bytes, stream, a, g, int(p.k_slots), p.span, kept);
 }
 

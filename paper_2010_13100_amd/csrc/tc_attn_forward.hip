@@ -154,6 +154,7 @@ __global__ __launch_bounds__(NW * 64, tile_waves<T>(DH, NW)) void k_attn_tile(
             to_scores<CAP>(a, a.table && !near ? far_bias(a, bias, rel) - sm.ref : -sm.ref, x[n]);
             if (near) add_bias(a, bias, rel, x[n]);
             if (k0 + 32 > lim_first || k0 + 32 > end) {
+                apart();
                 const int left = min(lim, end) - k0 - 4 * half;
 #pragma unroll
                 for (int r = 0; r < 16; r++) x[n][r] = reg_row(r) < left ? x[n][r] : -INFINITY;
@@ -334,6 +335,7 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
             for (int r = 0; r < 16; r++) x[r] += y[r];
         }
         if (kb + 32 > seen_first || kb + 32 > end) {
+            apart();
             const int left = lim - kb - 4 * half;
 #pragma unroll
             for (int r = 0; r < 16; r++) x[r] = reg_row(r) < left ? x[r] : -INFINITY;
