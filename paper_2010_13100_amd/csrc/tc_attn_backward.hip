@@ -143,26 +143,64 @@ __device__ __forceinline__ void add_distances(const Args &a, const f32x16 &ds, i
         dist[d + a.reach] += x;
 }
 
-// Gradient of the queries. A wavefront has 32 queries, the workgroup shares
-// tiles of BN keys and values. With NBUF = 2 the next tile arrives while one is
-// worked on; a lone wavefront, whose share of a tile is four times as large, has
-// no registers for that.
+// Orders what the threads that share a tile do to it.
+template <int WS>
+__device__ __forceinline__ void sync_tile() {
+    if (WS > 1)
+        __builtin_amdgcn_wave_barrier();  // a wavefront's own: LDS keeps its order
+    else
+        __syncthreads();
+}
+
+// Adds WS wavefronts' transposed blocks x of 32 rows (columns of the blocks) in
+// order, through sums[WS][32][DH] in LDS, and calls each(row, element, 4 sums).
+// All threads of the workgroup, after a barrier that ends other use of sums.
+template <int DH, int WS, class Each>
+__device__ __forceinline__ void add_waves(float *sums, const f32x16 *x, Each each) {
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, half = l >> 5;
+#pragma unroll
+    for (int db = 0; db < DH / 32; db++) {
+        store_block(sums + (wave * 32 + (l & 31)) * DH, x[db], 1.0f, db, DH);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 32 * (DH / 4); c += WS * 64) {
+        const int r = c / (DH / 4), d = (c % (DH / 4)) * 4;
+        f32x4 y = *reinterpret_cast<const f32x4 *>(sums + r * DH + d);
+#pragma unroll
+        for (int w = 1; w < WS; w++)
+            y += *reinterpret_cast<const f32x4 *>(sums + (w * 32 + r) * DH + d);
+        each(r, d, y);
+    }
+}
+
+// Gradient of the queries. A wavefront has 32 queries and the workgroup's NW
+// wavefronts share tiles of BN keys and values. Where that leaves most of the
+// chip idle, a workgroup has 32 queries and its WS wavefronts take tiles in turn,
+// each with tiles of its own; their sums are added in order at the end.
+//
+// With NBUF = 2 the next tile arrives while one is worked on; a wavefront with
+// tiles of its own, whose share of them is four times as large, has no registers
+// for that.
 //
 // delta = sum_j p_j dp_j is <grad_out, out>, but out has been rounded, and the
 // bias gradient adds up so many terms p*(dp - delta) that cancel that this
 // shows. The terms of a row add up to 0, so what they do add up to here is
 // the error of delta: k_attn_dkv gets the sum of the two, exact to fp32.
-template <class T, bool CAP, int DH, int NW, int BN, int NBUF>
-__global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_dq(Args a, Grads g,
-                                                                                    int slots) {
+template <class T, bool CAP, int DH, int NW, int WS, int BN, int NBUF>
+__global__ __launch_bounds__(NW *WS * 64, WS == 1 && sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_dq(
+    Args a, Grads g, int slots) {
+    static_assert(NW == 1 || WS == 1, "");
     typedef Tile<T, DH> Tl;
     const typename Tl::Lane ln = Tl::lane();
     constexpr int BM = NW * 32, NT = NW * 64, KS = DH / 16, DB = DH / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int first_bad;
-    T *tiles = reinterpret_cast<T *>(lds);  // [NBUF][keys, values][BN][DH]
-    float *bias = reinterpret_cast<float *>(tiles + NBUF * 2 * BN * DH);
+    __shared__ float rests[WS][32];
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, half = l >> 5;
+    const int turn = WS > 1 ? wave : 0, tid = WS > 1 ? l : threadIdx.x;
+    // [WS][NBUF][keys, values][BN][DH]
+    T *tiles = reinterpret_cast<T *>(lds) + turn * NBUF * 2 * BN * DH;
+    float *bias = reinterpret_cast<float *>(reinterpret_cast<T *>(lds) + WS * NBUF * 2 * BN * DH);
     const int id = blockIdx.x;
     const int kvh = id % a.kv_heads, h = kvh * a.group + (id / a.kv_heads) % a.group;
     int tile;
@@ -172,15 +210,15 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
     if (i0 >= s.qn) return;
     const int end = limit(a, s, min(i0 + BM, s.qn) - 1), block_first = limit(a, s, i0);
     const auto kv = KvOf<T, false>::make({g.k, g.v, {}, {}, 0}, s, kvh);
-    const int w0 = i0 + wave * 32, i = w0 + (l & 31);
+    const int w0 = i0 + (WS > 1 ? 0 : wave * 32), i = w0 + (l & 31);
     const int lim = limit(a, s, min(i, s.qn - 1));
     const int lim_first = limit(a, s, min(w0, s.qn - 1));
     const int lim_last = limit(a, s, min(w0 + 31, s.qn - 1));
     const int64_t t = s.q0 + min(i, s.qn - 1);
-    const int tid = threadIdx.x;
     Stage<T, T, DH, NT, BN> st;
     st.init(tid, a.dim);
-    if (end > 0) st.load(kv, 0, end, a.dim);
+    const int kb0 = turn * BN;
+    if (kb0 < end) st.load(kv, kb0, end, a.dim);
     if (a.table) load_bias(a, h, -(i0 + BM - 1 + s.shift), end - 1 - (i0 + s.shift), bias);
     if (threadIdx.x == 0) first_bad = INT32_MAX;
 
@@ -214,17 +252,17 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
     f32x16 acc[DB];
 #pragma unroll
     for (int db = 0; db < DB; db++) acc[db] = zero16();
-    if (end > 0) st.put(tiles, tiles + BN * DH);
+    if (kb0 < end) st.put(tiles, tiles + BN * DH);
     __syncthreads();
     int buf = 0;
-    for (int kb = 0; kb < end; kb += BN) {
+    for (int kb = kb0; kb < end; kb += WS * BN) {
         T *kt = tiles + buf * 2 * BN * DH, *vt = kt + BN * DH;
         if (min(kb + BN, end) > block_first) {  // some rows see less of the tile
             clean_tile<T, DH, NT, BN>(kt, tid, [&](int r) { atomicMin(&first_bad, kb + r); });
-            __syncthreads();
+            sync_tile<WS>();
         }
-        const bool more = kb + BN < end;
-        if (NBUF == 2 && more) st.load(kv, kb + BN, end, a.dim);
+        const bool more = kb + WS * BN < end;
+        if (NBUF == 2 && more) st.load(kv, kb + WS * BN, end, a.dim);
 #pragma unroll
         for (int n = 0; n < BN / 32; n++) {
             const int k0 = kb + 32 * n, rel = k0 - (w0 + s.shift);
@@ -263,8 +301,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
             }
         }
         if (NBUF == 1) {
-            if (more) st.load(kv, kb + BN, end, a.dim);
-            __syncthreads();
+            if (more) st.load(kv, kb + WS * BN, end, a.dim);
+            sync_tile<WS>();
         } else {
             buf ^= 1;
         }
@@ -272,63 +310,87 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn
             T *next = tiles + buf * 2 * BN * DH;
             st.put(next, next + BN * DH);
         }
-        __syncthreads();
+        sync_tile<WS>();
     }
     rest += __shfl_xor(rest, 32, kWave);
+    if (WS > 1) __syncthreads();
     const int bad = first_bad;
     if (bad < lim_last)
-        for (int r = 0; r < min(32, s.qn - w0); r++)
+        for (int r = turn; r < min(32, s.qn - w0); r += WS)
             if (limit(a, s, w0 + r) > bad) row_dq<T>(a, g, s, w0 + r, h);
-    if (i >= s.qn || lim > bad) return;
-    if (half == 0) g.delta[h * a.total_q + t] = delta + rest;
-    T *dp = static_cast<T *>(g.dq.data) + t * g.dq.token_stride + h * g.dq.head_stride;
+    T *dq = static_cast<T *>(g.dq.data) + s.q0 * g.dq.token_stride + h * g.dq.head_stride;
+    if constexpr (WS > 1) {
+        float *sums = reinterpret_cast<float *>(lds);  // [WS][32][DH]
+        if (half == 0) rests[wave][l] = rest;
+        add_waves<DH, WS>(sums, acc, [&](int r, int d, f32x4 y) {
+            const int q = i0 + r;
+            if (q >= s.qn || limit(a, s, q) > bad) return;
+            const float f = deriv_scale(a);
+            const float z[4] = {y[0] * f, y[1] * f, y[2] * f, y[3] * f};
+            if (d < a.dim) store4(dq + q * g.dq.token_stride + d, z);
+        });
+        if (wave == 0 && half == 0 && i < s.qn && lim <= bad) {
+            for (int w = 1; w < WS; w++) rest += rests[w][l];
+            g.delta[h * a.total_q + t] = delta + rest;
+        }
+    } else {
+        if (i >= s.qn || lim > bad) return;
+        if (half == 0) g.delta[h * a.total_q + t] = delta + rest;
 #pragma unroll
-    for (int db = 0; db < DB; db++) store_block(dp, acc[db], deriv_scale(a), db, a.dim);
+        for (int db = 0; db < DB; db++)
+            store_block(dq + i * g.dq.token_stride, acc[db], deriv_scale(a), db, a.dim);
+    }
 }
 
 // Gradients of the keys and values, and the bias gradient by distance. A
 // wavefront has 32 keys, the workgroup shares tiles of BQ queries and their
-// output gradients and takes the heads that share the keys one after another,
-// so that their sum needs no atomics. Blocks have queries as rows here (the
-// products that follow sum over them).
+// output gradients (or, with WS wavefronts, 32 keys; as in k_attn_dq) and takes the
+// heads that share the keys one after another, so that their sum needs no
+// atomics. Blocks have queries as rows here (the products that follow sum over
+// them).
 //
 // A workgroup takes every gridDim.y-th tile of its heads (all heads of a tile run
-// together, and a sequence's first tiles, which most queries see, first) and, with DIST, keeps
-// one sum per head, distance and wavefront in LDS throughout, so that the order
-// of the terms is fixed. Where those of all its heads do not fit (kept = 1) it
+// together, and a sequence's first tiles, which most queries see, first) and,
+// with DIST, keeps one sum per head, distance and wavefront in LDS throughout, so
+// that the order of the terms is fixed. Where those of all its heads do not fit (kept = 1) it
 // keeps one head's and adds them to its own row in the workspace after each.
 // It has all heads that share a key head (span = group), or one (span = 1) and
 // leaves its part of the sum over them to k_attn_sum_heads.
-template <class T, bool CAP, int DH, int NW, int BQ, bool DIST, int NBUF>
-__global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn_dkv(
+template <class T, bool CAP, int DH, int NW, int WS, int BQ, bool DIST, int NBUF>
+__global__ __launch_bounds__(NW *WS * 64, WS == 1 && sizeof(T) * DH <= 128 ? 2 : 1) void k_attn_dkv(
     Args a, Grads g, int slots, int span, int kept) {
+    static_assert(NW == 1 || WS == 1, "");
     typedef Tile<T, DH> Tl;
     const typename Tl::Lane ln = Tl::lane();
     constexpr int BM = NW * 32, NT = NW * 64, KS = DH / 16, DB = DH / 32;
+    constexpr int ALL = NW * WS, THREADS = ALL * 64;  // wavefronts and threads
     // the widest rows leave no registers for the values: they stay in LDS
     constexpr bool VLDS = sizeof(T) * DH > 256;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int last_bad;
-    __shared__ __attribute__((aligned(16))) float stat[NBUF][2][BQ];  // lse (in log 2) and delta
-    T *tiles = reinterpret_cast<T *>(lds);  // [NBUF][queries, output gradients][BQ][DH]
-    T *values = tiles + NBUF * 2 * BQ * DH;
+    __shared__ __attribute__((aligned(16))) float stats[WS][NBUF][2][BQ];  // lse (log 2), delta
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, half = l >> 5;
+    const int turn = WS > 1 ? wave : 0, tid = WS > 1 ? l : threadIdx.x;
+    // [WS][NBUF][queries, output gradients][BQ][DH]
+    T *tiles = reinterpret_cast<T *>(lds) + turn * NBUF * 2 * BQ * DH;
+    T *values = reinterpret_cast<T *>(lds) + WS * NBUF * 2 * BQ * DH;
     float *bias = reinterpret_cast<float *>(values + (VLDS ? BM * DH : 0));
-    const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, half = l >> 5;
+    auto &stat = stats[turn];
     const int h0 = blockIdx.x * span, kvh = h0 / a.group, width = 2 * a.reach + 1;
     float *skew = bias + (a.table ? 2 * (a.reach + kBiasPad) + 1 : 0) + wave * kSkewFloats;
-    float *dists = skew + (NW - wave) * kSkewFloats;  // [kept][NW][width]
+    float *dists = skew + (ALL - wave) * kSkewFloats;  // [kept][ALL][width]
     float far_left = 0.0f, far_right = 0.0f;
     if (DIST)
-        for (int d = threadIdx.x; d < kept * NW * width; d += NT) dists[d] = 0.0f;
+        for (int d = threadIdx.x; d < kept * ALL * width; d += THREADS) dists[d] = 0.0f;
     // the workgroup's sums of the head in dists + at into its row; with `add`
     // to what the row holds
     auto flush = [&](int h, int at, bool add) {
         __syncthreads();
         float *p = g.bias_part + (int64_t(h) * gridDim.y + blockIdx.y) * width;
-        for (int d = threadIdx.x; d < width; d += NT) {
+        for (int d = threadIdx.x; d < width; d += THREADS) {
             float x = dists[at + d];
 #pragma unroll
-            for (int w = 1; w < NW; w++) x += dists[at + w * width + d];
+            for (int w = 1; w < ALL; w++) x += dists[at + w * width + d];
             p[d] = add ? p[d] + x : x;
         }
     };
@@ -342,8 +404,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     const Seq s = seq_of(a, b, -1);
     const int j0 = tile * BM;
     if (j0 >= s.kn) continue;
-    const int w0 = j0 + wave * 32, j = w0 + (l & 31);
-    const int begin = first_query(a, s, j0) / BQ * BQ;
+    const int w0 = j0 + (WS > 1 ? 0 : wave * 32), j = w0 + (l & 31);
+    const int first = first_query(a, s, j0) / BQ * BQ, begin = first + turn * BQ;
     const int block_last = first_query(a, s, min(j0 + BM, s.kn) - 1);
     const int fq = first_query(a, s, min(j, s.kn - 1));
     const int fq_first = first_query(a, s, min(w0, s.kn - 1));
@@ -352,7 +414,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     if (threadIdx.x == 0) last_bad = -1;
 
     V8<T> kf[KS], vf[VLDS ? 1 : KS];
-    T *vt = values + wave * 32 * DH;
+    T *vt = values + (WS > 1 ? 0 : wave * 32 * DH);  // (the same of all WS)
     {
         const int64_t t = s.k0 + min(j, s.kn - 1);
         const T *kp = static_cast<const T *>(g.k.data) + t * g.k.token_stride + kvh * g.k.head_stride;
@@ -391,7 +453,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     };
     for (int hg = 0; hg < span; hg++) {
         const int h = h0 + hg;
-        float *dist = dists + ((kept > 1 ? hg : 0) * NW + wave) * width;
+        float *dist = dists + ((kept > 1 ? hg : 0) * ALL + wave) * width;
         qrow = static_cast<const T *>(g.q.data) + s.q0 * g.q.token_stride + h * g.q.head_stride;
         orow = static_cast<const T *>(g.grad_out.data) + s.q0 * g.grad_out.token_stride +
                h * g.grad_out.head_stride;
@@ -399,20 +461,20 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
         delta = g.delta + h * a.total_q + s.q0;
         if (begin < s.qn) fetch(begin);
         __syncthreads();  // the last head's tiles and bias have been read
-        if (a.table) load_bias(a, h, j0 - (s.qn - 1 + s.shift), j0 + BM - 1 - (begin + s.shift), bias);
+        if (a.table) load_bias(a, h, j0 - (s.qn - 1 + s.shift), j0 + BM - 1 - (first + s.shift), bias);
         if (begin < s.qn) put(0);
         __syncthreads();
         int buf = 0;
-        for (int qb = begin; qb < s.qn; qb += BQ) {
+        for (int qb = begin; qb < s.qn; qb += WS * BQ) {
             T *qt = tiles + buf * 2 * BQ * DH, *ot = qt + BQ * DH;
             if (qb < block_last) {  // some keys are not seen by all of the tile
                 const auto seen = [&](int r) { atomicMax(&last_bad, min(qb + r, s.qn - 1)); };
                 clean_tile<T, DH, NT, BQ>(qt, tid, seen);
                 clean_tile<T, DH, NT, BQ>(ot, tid, seen);
-                __syncthreads();
+                sync_tile<WS>();
             }
-            const bool more = qb + BQ < s.qn;
-            if (NBUF == 2 && more) fetch(qb + BQ);
+            const bool more = qb + WS * BQ < s.qn;
+            if (NBUF == 2 && more) fetch(qb + WS * BQ);
             const int now = buf;
 #pragma unroll
             for (int n = 0; n < BQ / 32; n++) {
@@ -478,13 +540,13 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
                 }
             }
             if (NBUF == 1) {
-                if (more) fetch(qb + BQ);
-                __syncthreads();
+                if (more) fetch(qb + WS * BQ);
+                sync_tile<WS>();
             } else {
                 buf ^= 1;
             }
             if (more) put(buf);
-            __syncthreads();
+            sync_tile<WS>();
         }
         if (DIST) {
             far_left = wave_sum(far_left);
@@ -498,35 +560,54 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
         if (DIST && kept < span) {
             flush(h, 0, begun);
             __syncthreads();
-            for (int d = threadIdx.x; d < NW * width; d += NT) dists[d] = 0.0f;
+            for (int d = threadIdx.x; d < ALL * width; d += THREADS) dists[d] = 0.0f;
         }
     }
     begun = true;
     __syncthreads();
     const int bad = last_bad;
     if (bad >= fq_first)
-        for (int r = 0; r < min(32, s.kn - w0); r++)
+        for (int r = turn; r < min(32, s.kn - w0); r += WS)
             if (first_query(a, s, w0 + r) <= bad) {
                 row_dkv<T>(a, g, s, w0 + r, h0, span);
                 if (DIST && l == 0) nan_seen = true;
             }
-    if (j < s.kn && fq > bad) {
-        const int64_t t = s.k0 + j;
-        if (g.part) {
-            float *kp = g.part + (h0 * g.total_k + t) * a.dim;
-            float *vp = kp + int64_t(a.heads) * g.total_k * a.dim;
+    // rows of this head's part, or of the gradients
+    const bool part = g.part != nullptr;
+    float *kpart = part ? g.part + (h0 * g.total_k + s.k0) * a.dim : nullptr;
+    float *vpart = part ? kpart + int64_t(a.heads) * g.total_k * a.dim : nullptr;
+    T *kout = static_cast<T *>(g.dk.data) + s.k0 * g.dk.token_stride + kvh * g.dk.head_stride;
+    T *vout = static_cast<T *>(g.dv.data) + s.k0 * g.dv.token_stride + kvh * g.dv.head_stride;
+    if constexpr (WS > 1) {
+        float *sums = reinterpret_cast<float *>(lds);  // [WS][32][DH]
+        auto store = [&](float *p, T *o, int64_t stride, float f, int r, int d, f32x4 y) {
+            const int jj = j0 + r;
+            if (jj >= s.kn || first_query(a, s, jj) <= bad || d >= a.dim) return;
+            const float z[4] = {y[0] * f, y[1] * f, y[2] * f, y[3] * f};
+            if (part)
+                store4(p + int64_t(jj) * a.dim + d, z);
+            else
+                store4(o + jj * stride + d, z);
+        };
+        add_waves<DH, WS>(sums, dk, [&](int r, int d, f32x4 y) {
+            store(kpart, kout, g.dk.token_stride, deriv_scale(a), r, d, y);
+        });
+        __syncthreads();
+        add_waves<DH, WS>(sums, dv, [&](int r, int d, f32x4 y) {
+            store(vpart, vout, g.dv.token_stride, 1.0f, r, d, y);
+        });
+    } else if (j < s.kn && fq > bad) {
+        if (part) {
 #pragma unroll
             for (int db = 0; db < DB; db++) {
-                store_block(kp, dk[db], deriv_scale(a), db, a.dim);
-                store_block(vp, dv[db], 1.0f, db, a.dim);
+                store_block(kpart + int64_t(j) * a.dim, dk[db], deriv_scale(a), db, a.dim);
+                store_block(vpart + int64_t(j) * a.dim, dv[db], 1.0f, db, a.dim);
             }
         } else {
-            T *kp = static_cast<T *>(g.dk.data) + t * g.dk.token_stride + kvh * g.dk.head_stride;
-            T *vp = static_cast<T *>(g.dv.data) + t * g.dv.token_stride + kvh * g.dv.head_stride;
 #pragma unroll
             for (int db = 0; db < DB; db++) {
-                store_block(kp, dk[db], deriv_scale(a), db, a.dim);
-                store_block(vp, dv[db], 1.0f, db, a.dim);
+                store_block(kout + j * g.dk.token_stride, dk[db], deriv_scale(a), db, a.dim);
+                store_block(vout + j * g.dv.token_stride, dv[db], 1.0f, db, a.dim);
             }
         }
     }
@@ -534,8 +615,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) * DH <= 128 ? 2 : 1) void k_attn
     if (!DIST) return;
     for (int hg = 0; hg < span; hg++) {
         if (kept == span) {
-            if (nan_seen) dists[(hg * NW + wave) * width + a.reach] = __builtin_nanf("");
-            flush(h0 + hg, hg * NW * width, false);
+            if (nan_seen) dists[(hg * ALL + wave) * width + a.reach] = __builtin_nanf("");
+            flush(h0 + hg, hg * ALL * width, false);
         } else {
             // no tile: zeros; otherwise what the last head left, zeros too
             if (nan_seen) dists[wave * width + a.reach] = __builtin_nanf("");
@@ -627,23 +708,57 @@ __global__ __launch_bounds__(kBlock) void k_bias_buckets(Args a, const float *pa
 
 // Tiles and workgroups of a call, from its sizes alone.
 struct Plan {
-    int q_waves, k_waves;  // of a workgroup of k_attn_dq, of k_attn_dkv
+    int q_waves, q_turns;  // of a workgroup of k_attn_dq: NW and WS
+    int k_waves, k_turns;  // of k_attn_dkv
     int64_t q_slots, k_slots;
     int span, parts;  // of k_attn_dkv: heads of a workgroup, workgroups of a head
+    int kept;         // heads whose sums by distance it keeps at a time
 };
+
+// Wavefronts take turns at tiles (WS > 1) up to this many 32-row tiles a CU.
+constexpr int kTurnsTiles = 4;
+
+constexpr size_t kMaxLds = 156 << 10;  // of 160 KB, the kernels' fixed arrays aside
+
+constexpr int dkv_queries(size_t elem, int dh, int nw) {
+    return nw == 1 || elem * dh > 256 ? 32 : 64;
+}
+
+// LDS of k_attn_dkv.
+size_t dkv_lds(const tc_attn &a, int nw, int ws, int kept) {
+    const size_t elem = a.dtype == TC_F32 ? 4 : 2, dh = a.head_dim <= 64 ? 64 : 128;
+    const size_t buffers = nw == 1 ? 1 : 2;
+    size_t n = ws * buffers * 2 * dkv_queries(elem, int(dh), nw) * dh * elem;
+    if (elem * dh > 256) n += nw * 32 * dh * elem;
+    if (a.bias_table)
+        n += sizeof(float) * (bias_entries(a.reach) + nw * ws * kSkewFloats +
+                              size_t(kept) * nw * ws * (2 * a.reach + 1));
+    return n;
+}
 
 Plan plan_of(const tc_attn &a) {
     Plan p{};
     const int64_t n = a.num_seqs > 0 ? a.num_seqs : 1;
     const int group = a.num_heads / a.num_kv_heads;
-    p.q_waves = a.max_q <= 32 || a.total_q / n <= 64 ? 1 : 4;
-    p.k_waves = a.max_k <= 32 || a.total_k / n <= 64 ? 1 : 4;
+    const int64_t cus = device_cus();
+    // tiles of 32 rows: few enough that a wavefront each leaves the chip idle?
+    const int64_t q32 = tile_slots(a.total_q, a.num_seqs, 32) * a.num_heads;
+    const int64_t k32 = tile_slots(a.total_k, a.num_seqs, 32) * a.num_heads;
+    p.q_turns = q32 <= kTurnsTiles * cus && a.max_k > 32 ? 4 : 1;
+    p.k_turns = k32 <= kTurnsTiles * cus && a.max_q > 32 ? 4 : 1;
+    p.q_waves = p.q_turns > 1 || a.max_q <= 32 || a.total_q / n <= 64 ? 1 : 4;
+    p.k_waves = p.k_turns > 1 || a.max_k <= 32 || a.total_k / n <= 64 ? 1 : 4;
+    if (dkv_lds(a, p.k_waves, p.k_turns, 1) > kMaxLds) p.k_waves = p.k_turns = 1;
     p.q_slots = tile_slots(a.total_q, a.num_seqs, 32 * p.q_waves);
     p.k_slots = tile_slots(a.total_k, a.num_seqs, 32 * p.k_waves);
-    const int64_t cus = device_cus();
-    p.span = p.k_slots * p.k_waves * a.num_kv_heads >= 16 * cus ? group : 1;
+    p.span = p.k_slots * p.k_waves * p.k_turns * a.num_kv_heads >= 16 * cus ? group : 1;
     const int64_t most = 8 * cus * p.span / a.num_heads + 1;
     p.parts = int(p.k_slots < most ? p.k_slots : most);
+    // the sums of all its heads in 32 KB and in LDS, or one's at a time
+    const bool all = size_t(p.span) * p.k_waves * p.k_turns * (2 * a.reach + 1) * sizeof(float) <=
+                         (32 << 10) &&
+                     dkv_lds(a, p.k_waves, p.k_turns, p.span) <= kMaxLds;
+    p.kept = all ? p.span : 1;
     return p;
 }
 
@@ -671,39 +786,47 @@ Space space_of(const tc_attn &a) {
     return s;
 }
 
-template <class T, bool CAP, int DH, int NW, bool DIST>
-void launch_dkv(const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
-    constexpr int NBUF = NW == 1 ? 1 : 2, BQ = NW == 1 || sizeof(T) * DH > 256 ? 32 : 64;
-    const size_t width = DIST ? (2 * a.reach + 1) * sizeof(float) : 0;
-    // sums by distance of all heads of a workgroup in 32 KB, or of one
-    const int kept = size_t(p.span) * NW * width <= (32 << 10) ? p.span : 1;
-    const size_t bytes = (NBUF * 2 * BQ + (sizeof(T) * DH > 256 ? NW * 32 : 0)) * DH * sizeof(T) +
-                         (a.table ? bias_entries(a.reach) * sizeof(float) : 0) +
-                         (DIST ? NW * kSkewFloats * sizeof(float) : 0) + kept * NW * width;
-    hipLaunchKernelGGL((k_attn_dkv<T, CAP, DH, NW, BQ, DIST, NBUF>), dim3(a.heads / p.span, p.parts),
-                       dim3(NW * 64), bytes, stream, a, g, int(p.k_slots), p.span, kept);
+template <class T, bool CAP, int DH, int NW, int WS, bool DIST>
+void launch_dkv(const tc_attn &t, const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
+    constexpr int NBUF = NW == 1 ? 1 : 2, BQ = dkv_queries(sizeof(T), DH, NW);
+    hipLaunchKernelGGL((k_attn_dkv<T, CAP, DH, NW, WS, BQ, DIST, NBUF>),
+                       dim3(a.heads / p.span, p.parts), dim3(NW * WS * 64),
+                       dkv_lds(t, NW, WS, p.kept), stream, a, g, int(p.k_slots), p.span, p.kept);
+}
+
+template <class T, bool CAP, int DH, bool DIST>
+void launch_dkv(const tc_attn &t, const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
+    if (p.k_turns > 1)
+        launch_dkv<T, CAP, DH, 1, 4, DIST>(t, a, p, g, stream);
+    else if (p.k_waves == 1)
+        launch_dkv<T, CAP, DH, 1, 1, DIST>(t, a, p, g, stream);
+    else
+        launch_dkv<T, CAP, DH, 4, 1, DIST>(t, a, p, g, stream);
+}
+
+template <class T, bool CAP, int DH, int NW, int WS, int BN, int NBUF>
+void launch_dq(const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
+    const size_t bytes = WS * NBUF * 2 * BN * DH * sizeof(T) +
+                         (a.table ? bias_entries(a.reach) * sizeof(float) : 0);
+    hipLaunchKernelGGL((k_attn_dq<T, CAP, DH, NW, WS, BN, NBUF>), dim3(unsigned(p.q_slots * a.heads)),
+                       dim3(NW * WS * 64), bytes, stream, a, g, int(p.q_slots));
 }
 
 template <class T, bool CAP, int DH>
 void launch(const tc_attn &t, const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
-    constexpr int BN = sizeof(T) == 4 ? 32 : 64;
-    const size_t bias = a.table ? bias_entries(a.reach) * sizeof(float) : 0;
     if (t.total_q > 0) {
-        const dim3 grid(unsigned(p.q_slots * a.heads));
-        if (p.q_waves == 1)
-            hipLaunchKernelGGL((k_attn_dq<T, CAP, DH, 1, 32, 1>), grid, dim3(64),
-                               2 * 32 * DH * sizeof(T) + bias, stream, a, g, int(p.q_slots));
+        if (p.q_turns > 1)
+            launch_dq<T, CAP, DH, 1, 4, 32, 1>(a, p, g, stream);
+        else if (p.q_waves == 1)
+            launch_dq<T, CAP, DH, 1, 1, 32, 1>(a, p, g, stream);
         else
-            hipLaunchKernelGGL((k_attn_dq<T, CAP, DH, 4, BN, 2>), grid, dim3(256),
-                               4 * BN * DH * sizeof(T) + bias, stream, a, g, int(p.q_slots));
+            launch_dq<T, CAP, DH, 4, 1, sizeof(T) == 4 ? 32 : 64, 2>(a, p, g, stream);
     }
     if (t.total_k > 0) {
-        if (p.k_waves == 1)
-            g.bias_part ? launch_dkv<T, CAP, DH, 1, true>(a, p, g, stream)
-                        : launch_dkv<T, CAP, DH, 1, false>(a, p, g, stream);
+        if (g.bias_part)
+            launch_dkv<T, CAP, DH, true>(t, a, p, g, stream);
         else
-            g.bias_part ? launch_dkv<T, CAP, DH, 4, true>(a, p, g, stream)
-                        : launch_dkv<T, CAP, DH, 4, false>(a, p, g, stream);
+            launch_dkv<T, CAP, DH, false>(t, a, p, g, stream);
         if (g.part) {
             const int64_t n = 2 * t.total_k * t.num_kv_heads * (t.head_dim / 4);
             hipLaunchKernelGGL((k_attn_sum_heads<T>),

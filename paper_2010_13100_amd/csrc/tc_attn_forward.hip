@@ -443,10 +443,12 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
 // Adds the splits of one row, where it has more than one: a wavefront per
 // (query, head).
 template <class T, bool PAGED>
-__global__ __launch_bounds__(kWave) void k_attn_join(Args a, Source src, Output<T> o,
+__global__ __launch_bounds__(kBlock) void k_attn_join(Args a, Source src, Output<T> o,
                                                                Split sp) {
-    const int l = threadIdx.x;
-    const int64_t row = blockIdx.x, t = row / a.heads, rows = a.total_q * a.heads;
+    const int l = threadIdx.x & 63;
+    const int64_t rows = a.total_q * a.heads, row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    const int64_t t = row / a.heads;
     const int h = int(row - t * a.heads);
     const int b = last_at_most(a.num_seqs, t, [&](int n) { return int64_t(a.q_off[n]); });
     const Seq s = seq_at<PAGED>(a, src, b);
@@ -546,8 +548,14 @@ Plan plan_of(const tc_attn &a) {
     Plan p{};
     const int group = a.num_heads / a.num_kv_heads;
     const int64_t rows = int64_t(a.max_q) * group;
-    p.few = rows <= 64 && a.max_k > 128;
     p.row_tiles = int((rows + 31) / 32);
+    // Few rows a key head over long keys, or so few rows that they leave most of
+    // the chip idle. Against k_attn_tile: 64 x 1 queries over 100 keys, 512
+    // workgroups, 12 us and 16; 16 x 200 of 2 heads, 208, 11 and 13; but 256 x 60 of
+    // 4 heads, 2048, 34 and 14; 2 x 2000 of 4 heads, 504, 72 and 55.
+    const int64_t few = int64_t(a.num_seqs) * a.num_kv_heads * p.row_tiles, cus = device_cus();
+    p.few = (rows <= 64 && a.max_k > 128) ||
+            (a.max_k > 32 && few <= (rows <= 32 ? 4 * cus : cus));
     const int64_t mean = a.num_seqs ? a.total_q / a.num_seqs : 0;
     p.waves = a.max_q <= 32 || mean <= 64 ? 1 : 4;
     p.blocks = p.few ? int64_t(a.num_seqs) * a.num_kv_heads * p.row_tiles
@@ -609,8 +617,8 @@ void launch(const tc_attn &t, const Args &a, const Plan &p, const Source &src, t
             hipLaunchKernelGGL((k_attn_join_many<T, PAGED>), dim3(rows, (a.dim + 31) / 32),
                                dim3(kBlock), 0, stream, a, src, o, sp);
         else
-            hipLaunchKernelGGL((k_attn_join<T, PAGED>), dim3(rows), dim3(kWave), 0, stream, a, src,
-                               o, sp);
+            hipLaunchKernelGGL((k_attn_join<T, PAGED>), dim3((rows + 3) / 4), dim3(kBlock), 0,
+                               stream, a, src, o, sp);
     }
 }
 

@@ -10,8 +10,9 @@
 // Both calls move every element once and compute almost nothing: bound by
 // memory. A lane group of dim/8 lanes (a power of two, up to 16) has a row, 8
 // elements a lane, so that loads and stores are 16 or 32 bytes and a row's
-// maximum is a few shuffles; the token's place (its sequence by a search
-// over the offsets, then its page) is found once for its kv_heads rows.
+// maximum is a few shuffles. A workgroup has a run of tokens, kTokens of them at
+// a time in each lane group, so that many loads are under way; the sequence of
+// the run's first token is found by a search, that of the others by walking on.
 #include "tc_attn.h"
 
 namespace tc {
@@ -54,19 +55,6 @@ __device__ __forceinline__ void store8(bf16 *p, const float *x) {
     *reinterpret_cast<bf16x8 *>(p) = a;
 }
 
-// Where token t's row of head h lies in the cache: false if it has no place.
-__device__ __forceinline__ bool place(const tc_cache &c, int num_seqs, const int32_t *offsets,
-                                      int64_t t, int64_t &data, int64_t &slot) {
-    const int b = seq_of_token(offsets, num_seqs, t);
-    const int64_t pos = int64_t(c.lens[b]) - (offsets[b + 1] - t);
-    if (pos < 0 || pos >= int64_t(c.max_pages) * c.page_size) return false;
-    const int64_t p = pos / c.page_size, s = pos - p * c.page_size;
-    const int64_t page = c.page_table[int64_t(b) * c.max_pages + p];
-    data = page * c.page_stride + s * c.slot_stride;
-    slot = page * c.page_size + s;
-    return true;
-}
-
 // 8-bit form of one row's 8 elements in this lane: LANES lanes have the row.
 template <int LANES>
 __device__ __forceinline__ u32x2 quantise(const float *x, uint32_t &e_out) {
@@ -76,8 +64,12 @@ __device__ __forceinline__ u32x2 quantise(const float *x, uint32_t &e_out) {
 #pragma unroll
     for (int i = 0; i < 8; i++)
         top = max(top, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, uint32_t(__shfl_xor(top, o, kWave)));
+    // over the row's lanes, without LDS: neighbours, pairs, then mirrored halves
+    // and rows of 16
+    if (LANES > 1) top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0xb1, 0xf, 0xf, true)));
+    if (LANES > 2) top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0x4e, 0xf, 0xf, true)));
+    if (LANES > 4) top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0x141, 0xf, 0xf, true)));
+    if (LANES > 8) top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0x140, 0xf, 0xf, true)));
     if (top >= 0x7f800000u) {
         e_out = 255;
         return u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
@@ -113,51 +105,109 @@ __device__ __forceinline__ void dequantise(u32x2 r, uint32_t e, float *x) {
     }
 }
 
-// One lane group per (token, k or v, head): consecutive groups have a
-// token's heads, then its other array, so that a wavefront's tokens are few.
+constexpr int kTokens = 4;
+
+// Read in place of rows that have no place: loads under a condition would wait
+// for one another.
+__device__ __attribute__((aligned(16))) const uint32_t kNoRow[8] = {};
+
+// Lane group r of a workgroup has row r % per of every (256 / LANES / per)-th
+// token of the run (per: a token's rows, k and v of every head), or where a token
+// has more rows than there are groups, every such row of each token.
 template <class T, bool FP8, bool WRITE, int LANES>
-__global__ __launch_bounds__(kBlock) void k_cache_rows(tc_cache c, int num_seqs,
+__global__ __launch_bounds__(kBlock) void k_cache_rows(tc_cache c, Divider page_size, int num_seqs,
                                                        const int32_t *__restrict__ offsets,
-                                                       int64_t total, tc_rows k, tc_rows v) {
-    const int lane = threadIdx.x % LANES;
+                                                       int32_t total, int32_t run, tc_rows k,
+                                                       tc_rows v) {
+    constexpr int GROUPS = kBlock / LANES;
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     const int per = 2 * c.num_kv_heads;
-    const int64_t groups = int64_t(gridDim.x) * (kBlock / LANES);
-    const int64_t rows = total * per;
-    for (int64_t r = int64_t(blockIdx.x) * (kBlock / LANES) + threadIdx.x / LANES; r < rows;
-         r += groups) {
-        const int64_t t = r / per;
-        const int which = int(r - t * per), h = which >> 1;
-        const bool is_v = which & 1;
-        const tc_rows &rw = is_v ? v : k;
-        T *row = static_cast<T *>(rw.data) + t * rw.token_stride + h * rw.head_stride + lane * 8;
-        const bool mine = lane * 8 < c.head_dim;
-        int64_t data, slot;
-        const bool held = place(c, num_seqs, offsets, t, data, slot);
-        data += h * c.head_stride + lane * 8;
-        slot = slot * c.num_kv_heads + h;
-        float x[8] = {};
-        if (WRITE) {
-            if (!held) continue;
-            if (mine) load8(row, x);
-            if (FP8) {
-                uint32_t e;
-                const u32x2 q = quantise<LANES>(x, e);
-                if (mine)
-                    *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(is_v ? c.v : c.k) + data) = q;
-                if (lane == 0) (is_v ? c.v_exp : c.k_exp)[slot] = uint8_t(e);
-            } else if (mine) {
-                store8(static_cast<T *>(is_v ? c.v : c.k) + data, x);
+    const int side = max(GROUPS / per, 1);  // tokens side by side
+    const int first = blockIdx.x * run, end = min(first + run, total);
+    const bool mine = lane * 8 < c.head_dim;
+    if (group / min(per, GROUPS) >= side) return;  // a remainder of groups
+    const int64_t places = int64_t(c.max_pages) * c.page_size;
+    int b = seq_of_token(offsets, num_seqs, first);
+    int next = offsets[b + 1];
+    for (int t0 = first + (per < GROUPS ? group / per : 0); t0 < end; t0 += side * kTokens) {
+        bool in[kTokens], held[kTokens];
+        int64_t data[kTokens], slot[kTokens];
+#pragma unroll
+        for (int n = 0; n < kTokens; n++) {
+            const int t = t0 + n * side;
+            in[n] = t < end;
+            held[n] = false;
+            data[n] = slot[n] = 0;
+            if (!in[n]) continue;
+            while (t >= next && b + 1 < num_seqs) {
+                b++;
+                next = offsets[b + 1];
             }
-        } else {
-            if (held && mine) {
-                if (FP8)
-                    dequantise(*reinterpret_cast<const u32x2 *>(
-                                   static_cast<const uint8_t *>(is_v ? c.v : c.k) + data),
-                               (is_v ? c.v_exp : c.k_exp)[slot], x);
-                else
-                    load8(static_cast<const T *>(is_v ? c.v : c.k) + data, x);
+            const int64_t pos = int64_t(c.lens[b]) - (next - t);
+            held[n] = pos >= 0 && pos < places;
+            if (!held[n]) continue;
+            const int p = divide(int(pos), page_size), s = int(pos) - p * c.page_size;
+            const int64_t page = c.page_table[int64_t(b) * c.max_pages + p];
+            data[n] = page * c.page_stride + s * c.slot_stride + lane * 8;
+            slot[n] = (page * c.page_size + s) * c.num_kv_heads;
+        }
+        for (int which = group % min(per, GROUPS); which < per; which += GROUPS) {
+            const int h = which >> 1;
+            const bool is_v = which & 1;
+            const tc_rows &rw = is_v ? v : k;
+            T *row = static_cast<T *>(rw.data) + h * rw.head_stride + (mine ? lane * 8 : 0);
+            void *base = is_v ? c.v : c.k;
+            uint8_t *exps = is_v ? c.v_exp : c.k_exp;
+            float x[kTokens][8];
+            if (WRITE) {
+#pragma unroll
+                for (int n = 0; n < kTokens; n++)
+                    load8(row + int64_t(min(t0 + n * side, end - 1)) * rw.token_stride, x[n]);
+                if (FP8) {
+#pragma unroll
+                    for (int n = 0; n < kTokens; n++) {
+#pragma unroll
+                        for (int e = 0; e < 8; e++) x[n][e] = mine ? x[n][e] : 0.0f;
+                        uint32_t e;
+                        const u32x2 q = quantise<LANES>(x[n], e);
+                        if (!held[n]) continue;
+                        const int64_t at = data[n] + h * c.head_stride;
+                        if (mine) *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(base) + at) = q;
+                        if (lane == 0) exps[slot[n] + h] = uint8_t(e);
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < kTokens; n++)
+                        if (held[n] && mine)
+                            store8(static_cast<T *>(base) + data[n] + h * c.head_stride, x[n]);
+                }
+            } else {
+                if (FP8) {
+                    u32x2 q[kTokens];
+                    uint32_t e[kTokens];
+#pragma unroll
+                    for (int n = 0; n < kTokens; n++) {
+                        const auto *none = reinterpret_cast<const uint8_t *>(kNoRow);
+                        const int64_t at = data[n] + h * c.head_stride;
+                        q[n] = *reinterpret_cast<const u32x2 *>(
+                            held[n] && mine ? static_cast<const uint8_t *>(base) + at : none);
+                        e[n] = *(held[n] ? exps + slot[n] + h : none);
+                    }
+#pragma unroll
+                    for (int n = 0; n < kTokens; n++) dequantise(q[n], e[n], x[n]);
+                } else {
+#pragma unroll
+                    for (int n = 0; n < kTokens; n++)
+                        load8(held[n] && mine
+                                  ? static_cast<const T *>(base) + data[n] + h * c.head_stride
+                                  : reinterpret_cast<const T *>(kNoRow),
+                              x[n]);
+                }
+#pragma unroll
+                for (int n = 0; n < kTokens; n++)
+                    if (in[n] && mine)
+                        store8(row + int64_t(t0 + n * side) * rw.token_stride, x[n]);
             }
-            if (mine) store8(row, x);
         }
     }
 }
@@ -167,12 +217,20 @@ void launch_rows(const tc_cache &c, int num_seqs, const int32_t *offsets, int64_
                  tc_rows v, hipStream_t stream) {
     int lanes = 1;
     while (lanes * 8 < c.head_dim) lanes *= 2;
-    const int64_t rows = total * 2 * c.num_kv_heads;
-    const dim3 grid(grid_for(rows, kBlock / lanes, int64_t(device_cus()) * 8 * 4));
-#define TC_LAUNCH(L)                                                                             \
-    case L:                                                                                      \
-        hipLaunchKernelGGL((k_cache_rows<T, FP8, WRITE, L>), grid, dim3(kBlock), 0, stream, c,   \
-                           num_seqs, offsets, total, k, v);                                      \
+    // a run is what a workgroup has under way at a time, or more so that a few
+    // workgroups a CU have them all
+    const int groups = kBlock / lanes, per = 2 * c.num_kv_heads;
+    const int64_t once = int64_t(groups / per > 1 ? groups / per : 1) * kTokens;
+    const int64_t most = int64_t(device_cus()) * 16;
+    int64_t run = (total + most - 1) / most;
+    run = (run + once - 1) / once * once;
+    if (total < 2 * most) run = once / kTokens;  // few tokens: one in each lane group
+    const dim3 grid(unsigned((total + run - 1) / run));
+    const Divider d = make_divider(uint32_t(c.page_size));
+#define TC_LAUNCH(L)                                                                               \
+    case L:                                                                                        \
+        hipLaunchKernelGGL((k_cache_rows<T, FP8, WRITE, L>), grid, dim3(kBlock), 0, stream, c, d,  \
+                           num_seqs, offsets, int32_t(total), int32_t(run), k, v);                 \
         break;
     switch (lanes) {
         TC_LAUNCH(1) TC_LAUNCH(2) TC_LAUNCH(4) TC_LAUNCH(8) TC_LAUNCH(16)
@@ -188,8 +246,8 @@ tc_status cache_call(const char *fn, bool write, const tc_cache *c, int32_t dtyp
                "%s: dtype %d is neither TC_F32 nor TC_BF16", fn, dtype);
     const tc_status st = check_cache(fn, c, dtype);
     if (st != TC_OK) return st;
-    TC_REQUIRE(num_seqs >= 0 && total >= 0 && total < (int64_t(1) << 31), TC_ERR_INVALID_ARG,
-               "%s: num_seqs and total must not be negative, total below 2^31", fn);
+    TC_REQUIRE(num_seqs >= 0 && total >= 0 && total < (int64_t(1) << 30), TC_ERR_INVALID_ARG,
+               "%s: num_seqs and total must not be negative, total below 2^30", fn);
     if (total == 0) return TC_OK;
     TC_REQUIRE(num_seqs > 0, TC_ERR_INVALID_ARG, "%s: rows but no sequences", fn);
     TC_REQUIRE(offsets && c->page_table && c->lens, TC_ERR_INVALID_ARG, "%s: null pointer", fn);
