@@ -72,6 +72,23 @@ inline Args make_args(const tc_attn &a) {
     return r;
 }
 
+// Whether rows of short sequences go side by side into tiles of 32 rather than
+// each sequence's into its own: where the chip is full (side by side there are
+// fewer wavefronts, with more tiles each) and the sequences' own tiles would be
+// filled to less than `percent`. Measured with 160k rows of 2 heads of 64, side by
+// side and own, us:
+//   rows a sequence       3        8        13       20       28       40       45
+//   forward bf16       50/180    46/81    50/55    50/43      -      51/54    53/51
+//   training bf16    233/1476  241/538  264/418  246/329  261/230  239/343  273/279
+//   training fp32    492/3126  468/1260 555/849  503/643  547/480  501/733  585/661
+// and 256 x 20 of one head, training fp32, 55/46; 256 x 60 of 4, bf16, 106/78.
+constexpr int kPackForward = 60, kPackBackward = 80;
+inline bool pack_rows(int64_t rows, int64_t num_seqs, int heads, int percent) {
+    if (num_seqs <= 0 || (rows / 32 + num_seqs) * heads <= int64_t(device_cus()) * 16) return false;
+    const int64_t tiles = (rows + 32 * num_seqs - 1) / (32 * num_seqs);
+    return rows * 100 < tiles * 32 * num_seqs * percent;
+}
+
 // One sequence.
 struct Seq {
     int32_t b, qn, kn, shift, prefix;  // pos_i = i + shift

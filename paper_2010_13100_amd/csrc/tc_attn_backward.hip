@@ -143,6 +143,35 @@ __device__ __forceinline__ void add_distances(const Args &a, const f32x16 &ds, i
         dist[d + a.reach] += x;
 }
 
+// Operands of this lane's query t, and <grad_out, out> of it.
+template <class T, int DH>
+__device__ __forceinline__ float load_rows_and_delta(const Args &a, const Grads &g, int64_t t, int h,
+                                                     V8<T> *qf, V8<T> *of) {
+    const int l = threadIdx.x & 63, half = l >> 5;
+    const T *qp = static_cast<const T *>(g.q.data) + t * g.q.token_stride + h * g.q.head_stride;
+    const T *gp = static_cast<const T *>(g.grad_out.data) + t * g.grad_out.token_stride +
+                  h * g.grad_out.head_stride;
+    const T *op = static_cast<const T *>(g.out.data) + t * g.out.token_stride +
+                  h * g.out.head_stride;
+    // the diagonal of a product of the same form as <grad_out, v> later: where
+    // one key has all the weight, out is v, and their difference is 0 to the last
+    // bit
+    f32x16 x = zero16();
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ks++) {
+        const int c = 2 * ks + half;
+        qf[ks] = chunk_of(qp, c, a.dim);
+        of[ks] = chunk_of(gp, c, a.dim);
+        x = mma(chunk_of(op, c, a.dim), of[ks], x);
+    }
+    float delta = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; r++) delta = 4 * half + reg_row(r) == (l & 31) ? x[r] : delta;
+    // the other half has the entry if this one does not
+    const float other = __shfl_xor(delta, 32, kWave);
+    return ((l & 31) >> 2 & 1) == half ? delta : other;
+}
+
 // Orders what the threads that share a tile do to it.
 template <int WS>
 __device__ __forceinline__ void sync_tile() {
@@ -223,30 +252,8 @@ __global__ __launch_bounds__(NW *WS * 64, WS == 1 && sizeof(T) * DH <= 256 ? 2 :
     if (threadIdx.x == 0) first_bad = INT32_MAX;
 
     V8<T> qf[KS], of[KS];
-    float delta = 0.0f, rest = 0.0f;
-    {
-        const T *qp = static_cast<const T *>(g.q.data) + t * g.q.token_stride + h * g.q.head_stride;
-        const T *gp = static_cast<const T *>(g.grad_out.data) + t * g.grad_out.token_stride +
-                      h * g.grad_out.head_stride;
-        const T *op = static_cast<const T *>(g.out.data) + t * g.out.token_stride +
-                      h * g.out.head_stride;
-        // <grad_out, out> as the diagonal of a product of the same form as
-        // <grad_out, v> below: where one key has all the weight, out is v, and
-        // their difference is 0 to the last bit
-        f32x16 x = zero16();
-#pragma unroll
-        for (int ks = 0; ks < KS; ks++) {
-            const int c = 2 * ks + half;
-            qf[ks] = chunk_of(qp, c, a.dim);
-            of[ks] = chunk_of(gp, c, a.dim);
-            x = mma(chunk_of(op, c, a.dim), of[ks], x);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; r++) delta = 4 * half + reg_row(r) == (l & 31) ? x[r] : delta;
-        // the other half has the entry if this one does not
-        const float other = __shfl_xor(delta, 32, kWave);
-        delta = ((l & 31) >> 2 & 1) == half ? delta : other;
-    }
+    const float delta = load_rows_and_delta<T, DH>(a, g, t, h, qf, of);
+    float rest = 0.0f;
     const float lse2 = g.lse[h * a.total_q + t] * kLog2e;
 
     f32x16 acc[DB];
@@ -340,6 +347,108 @@ __global__ __launch_bounds__(NW *WS * 64, WS == 1 && sizeof(T) * DH <= 256 ? 2 :
         for (int db = 0; db < DB; db++)
             store_block(dq + i * g.dq.token_stride, acc[db], deriv_scale(a), db, a.dim);
     }
+}
+
+// The same for 32 queries of short sequences, side by side; a wavefront each.
+template <class T, bool CAP, int DH>
+__global__ __launch_bounds__(kWave, sizeof(T) * DH <= 256 ? 2 : 1) void k_pack_dq(Args a, Grads g) {
+    typedef Tile<T, DH> Tl;
+    const typename Tl::Lane ln = Tl::lane();
+    constexpr int KS = DH / 16, DB = DH / 32;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int sh[kWave];
+    T *kt = reinterpret_cast<T *>(lds), *vt = kt + 32 * DH;
+    float *bias = reinterpret_cast<float *>(vt + 32 * DH);
+    const int id = blockIdx.x, l = threadIdx.x, half = l >> 5;
+    const int kvh = id % a.kv_heads, h = kvh * a.group + (id / a.kv_heads) % a.group;
+    const int t0 = id / a.heads * 32, last = int(a.total_q) - 1;
+    const int t = min(t0 + (l & 31), last);
+    const int b = seq_of_lane(a.q_off, a.num_seqs, t, sh);
+    int lo, hi, pos;  // keys that this lane's query sees, and its place among them
+    {
+        const Seq s = seq_of(a, b, -1);
+        const int i = t - int(s.q0);
+        lo = int(s.k0);
+        hi = lo + limit(a, s, i);
+        pos = lo + i + s.shift;
+    }
+    const int begin = __builtin_amdgcn_readlane(lo, 0), end = __builtin_amdgcn_readlane(hi, 31);
+    const int lo_max = __builtin_amdgcn_readlane(lo, 31), hi_min = __builtin_amdgcn_readlane(hi, 0);
+    Seq all{};
+    const auto kv = KvOf<T, false>::make({g.k, g.v, {}, {}, 0}, all, kvh);
+    Stage<T, T, DH, kWave, 32> st;
+    st.init(l, a.dim);
+    if (begin < end) st.load(kv, begin, end, a.dim);
+
+    V8<T> qf[KS], of[KS];
+    const float delta = load_rows_and_delta<T, DH>(a, g, t, h, qf, of);
+    const float lse2 = g.lse[h * a.total_q + t] * kLog2e;
+    float rest = 0.0f;
+    if (a.table) load_bias(a, h, wave_min(lo - pos), -wave_min(pos + 1 - hi), bias);
+    f32x16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; db++) acc[db] = zero16();
+    bool bad = false;  // this lane's query sees a key that was cleaned
+    for (int kb = begin; kb < end; kb += 32) {
+        const bool part = kb < lo_max || kb + 32 > hi_min;  // some rows see less of the tile
+        __builtin_amdgcn_wave_barrier();
+        st.put(kt, vt);
+        __builtin_amdgcn_wave_barrier();
+        if (part) {
+            bool any = false;
+#pragma unroll
+            for (int n = 0; n < st.IT; n++) any |= not_finite(st.a[n].x);
+            if (__any(any))
+                bad |= meets(clean_mask<T, DH>(kt, reinterpret_cast<uint32_t *>(sh)), kb, lo, hi);
+        }
+        if (kb + 32 < end) st.load(kv, kb + 32, end, a.dim);
+        f32x16 x = zero16(), dp = zero16();
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) {
+            x = mma(Tl::rows(kt, ln, 0, ks), qf[ks], x);
+            dp = mma(Tl::rows(vt, ln, 0, ks), of[ks], dp);
+        }
+        float c0 = -lse2;
+        const bool near = a.table && __any(kb + 31 - pos > -a.reach && kb - pos < a.reach);
+        if (a.table && !near) c0 += bias[kb < pos ? 0 : 2 * (a.reach + kBiasPad)];
+        const Scores sc = scores_of<CAP>(a, c0, x);
+        x = sc.x;
+        if (near) add_bias_at(a, bias, kb, pos, x);
+#pragma unroll
+        for (int r = 0; r < 16; r++) x[r] = exp2_fast(x[r]) * (dp[r] - delta);
+        if (part) {
+            apart();
+            const int from = lo - kb - 4 * half, to = hi - kb - 4 * half;
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                x[r] = reg_row(r) >= from && reg_row(r) < to ? x[r] : 0.0f;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r++) rest += x[r];
+        if (CAP) {
+#pragma unroll
+            for (int r = 0; r < 16; r++) x[r] *= sc.f[r];
+        }
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            V8<T> p;
+            pack(x, u, p);
+#pragma unroll
+            for (int db = 0; db < DB; db++)
+                acc[db] = mma(Tl::cols(kt, ln, 16 * u, db), p, acc[db]);
+        }
+    }
+    rest += __shfl_xor(rest, 32, kWave);
+    for (uint64_t todo = __ballot(bad && half == 0); todo; todo &= todo - 1) {
+        const int r = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+        const Seq s = seq_of(a, __builtin_amdgcn_readlane(b, r), -1);
+        if (t0 + r <= last) row_dq<T>(a, g, s, t0 + r - int(s.q0), h);
+    }
+    if (t0 + (l & 31) > last || bad) return;
+    if (half == 0) g.delta[h * a.total_q + t] = delta + rest;
+    T *dq = static_cast<T *>(g.dq.data) + t * g.dq.token_stride + h * g.dq.head_stride;
+#pragma unroll
+    for (int db = 0; db < DB; db++) store_block(dq, acc[db], deriv_scale(a), db, a.dim);
 }
 
 // Gradients of the keys and values, and the bias gradient by distance. A
@@ -625,6 +734,218 @@ __global__ __launch_bounds__(NW *WS * 64, WS == 1 && sizeof(T) * DH <= 128 ? 2 :
     }
 }
 
+// The same for 32 keys of short sequences, side by side; a wavefront each.
+template <class T, bool CAP, int DH, bool DIST>
+__global__ __launch_bounds__(kWave, sizeof(T) * DH <= 128 ? 2 : 1) void k_pack_dkv(
+    Args a, Grads g, int tiles, int span, int kept) {
+    typedef Tile<T, DH> Tl;
+    const typename Tl::Lane ln = Tl::lane();
+    constexpr int KS = DH / 16, DB = DH / 32;
+    constexpr bool VLDS = sizeof(T) * DH > 256;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int sh[kWave];
+    __shared__ __attribute__((aligned(16))) float stat[2][32];  // lse (in log 2) and delta
+    T *qt = reinterpret_cast<T *>(lds), *ot = qt + 32 * DH, *vt = ot + 32 * DH;
+    float *bias = reinterpret_cast<float *>(vt + (VLDS ? 32 * DH : 0));
+    const int l = threadIdx.x, half = l >> 5;
+    const int h0 = blockIdx.x * span, kvh = h0 / a.group, width = 2 * a.reach + 1;
+    float *skew = bias + (a.table ? 2 * (a.reach + kBiasPad) + 1 : 0);
+    float *dists = skew + kSkewFloats;  // [kept][width]
+    float far_left = 0.0f, far_right = 0.0f;
+    if (DIST)
+        for (int d = l; d < kept * width; d += kWave) dists[d] = 0.0f;
+    // a head's sums into the workgroup's row; with `add` to what the row holds
+    auto flush = [&](int h, const float *p, bool add) {
+        __builtin_amdgcn_wave_barrier();
+        float *row = g.bias_part + (int64_t(h) * gridDim.y + blockIdx.y) * width;
+        for (int d = l; d < width; d += kWave) row[d] = add ? row[d] + p[d] : p[d];
+        __builtin_amdgcn_wave_barrier();
+    };
+    bool begun = false, nan_seen = false;
+    Stage<T, T, DH, kWave, 32> st;
+    st.init(l, a.dim);
+    const int last = int(g.total_k) - 1;
+
+    for (int tile = blockIdx.y; tile < tiles; tile += int(gridDim.y)) {
+        const int t0 = tile * 32, t = min(t0 + (l & 31), last);
+        const int b = seq_of_lane(a.k_off, a.num_seqs, t, sh);
+        // queries that see this lane's key; its distance from query i is kpos - i
+        int lo, hi, kpos;
+        {
+            const Seq s = seq_of(a, b, -1);
+            const int j = t - int(s.k0);
+            lo = int(s.q0) + first_query(a, s, j);
+            hi = int(s.q0) + s.qn;
+            kpos = j + int(s.q0) - s.shift;
+        }
+        const int begin = __builtin_amdgcn_readlane(lo, 0), end = __builtin_amdgcn_readlane(hi, 31);
+        const int lo_max = __builtin_amdgcn_readlane(lo, 31);
+        const int hi_min = __builtin_amdgcn_readlane(hi, 0);
+        const bool real = t0 + (l & 31) <= last;  // keys past the last one repeat it
+
+        V8<T> kf[KS], vf[VLDS ? 1 : KS];
+        const T *kp = static_cast<const T *>(g.k.data) + t * g.k.token_stride + kvh * g.k.head_stride;
+        const T *vp = static_cast<const T *>(g.v.data) + t * g.v.token_stride + kvh * g.v.head_stride;
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) {
+            kf[ks] = chunk_of(kp, 2 * ks + half, a.dim);
+            const V8<T> v = chunk_of(vp, 2 * ks + half, a.dim);
+            if (VLDS)
+                Tl::put(vt, l & 31, 2 * ks + half, v);
+            else
+                vf[VLDS ? 0 : ks] = v;
+        }
+        f32x16 dk[DB], dv[DB];
+#pragma unroll
+        for (int db = 0; db < DB; db++) dk[db] = dv[db] = zero16();
+        bool bad = false;  // a query that sees this lane's key was cleaned
+        const int d_lo = wave_min(kpos + 1 - hi), d_hi = -wave_min(lo - kpos);
+
+        for (int hg = 0; hg < span; hg++) {
+            const int h = h0 + hg;
+            float *dist = dists + (kept > 1 ? hg : 0) * width;
+            const T *qrow = static_cast<const T *>(g.q.data) + h * g.q.head_stride;
+            const T *orow = static_cast<const T *>(g.grad_out.data) + h * g.grad_out.head_stride;
+            const float *lse = g.lse + h * a.total_q, *delta = g.delta + h * a.total_q;
+            float lse_r = 0.0f, delta_r = 0.0f;
+            auto fetch = [&](int qb) {
+                st.load_rows(qrow, orow, g.q.token_stride, g.grad_out.token_stride, qb, end - 1);
+                const int i = min(qb + (l & 31), end - 1);
+                lse_r = lse[i] * kLog2e;
+                delta_r = delta[i];
+            };
+            if (begin < end) fetch(begin);
+            __builtin_amdgcn_wave_barrier();
+            if (a.table) load_bias(a, h, d_lo, d_hi, bias);
+            for (int qb = begin; qb < end; qb += 32) {
+                const bool part = qb < lo_max || qb + 32 > hi_min;  // some keys see less of it
+                __builtin_amdgcn_wave_barrier();
+                st.put(qt, ot);
+                stat[half][l & 31] = half ? delta_r : lse_r;
+                __builtin_amdgcn_wave_barrier();
+                if (part) {
+                    bool any = false;
+#pragma unroll
+                    for (int n = 0; n < st.IT; n++) any |= not_finite(st.a[n].x) | not_finite(st.b[n].x);
+                    if (__any(any)) {
+                        uint32_t *mask = reinterpret_cast<uint32_t *>(sh);
+                        const uint32_t m = clean_mask<T, DH>(qt, mask);
+                        bad |= meets(m | clean_mask<T, DH>(ot, mask), qb, lo, hi);
+                    }
+                }
+                if (qb + 32 < end) fetch(qb + 32);
+                f32x16 x = zero16(), dp = zero16();
+#pragma unroll
+                for (int ks = 0; ks < KS; ks++) {
+                    x = mma(Tl::rows(qt, ln, 0, ks), kf[ks], x);
+                    dp = mma(Tl::rows(ot, ln, 0, ks),
+                             VLDS ? Tl::rows(vt, ln, 0, ks) : vf[VLDS ? 0 : ks], dp);
+                }
+                float c0 = 0.0f;
+                const bool near = a.table && __any(kpos - qb > -a.reach && kpos - qb - 31 < a.reach);
+                if (a.table && !near) c0 = bias[kpos < qb ? 0 : 2 * (a.reach + kBiasPad)];
+                const Scores sc = scores_of<CAP>(a, c0, x);
+                x = sc.x;
+                if (near) add_bias_queries_at(a, bias, qb, kpos, x);
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    const f32x4 sum = *reinterpret_cast<const f32x4 *>(&stat[0][8 * c + 4 * half]);
+                    const f32x4 del = *reinterpret_cast<const f32x4 *>(&stat[1][8 * c + 4 * half]);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int r = 4 * c + e;
+                        x[r] = exp2_fast(x[r] - sum[e]);
+                        dp[r] = x[r] * (dp[r] - del[e]);
+                    }
+                }
+                if (part || qb + 32 > end) {
+                    apart();
+                    const int from = lo - qb - 4 * half, to = hi - qb - 4 * half;
+#pragma unroll
+                    for (int r = 0; r < 16; r++) {
+                        const bool in = reg_row(r) >= from && reg_row(r) < to;
+                        x[r] = in ? x[r] : 0.0f;
+                        dp[r] = in ? dp[r] : 0.0f;
+                    }
+                }
+                if (DIST) {
+                    // keys of one sequence are in line; most often all are
+                    const int off = kpos - (t0 + (l & 31));
+                    for (uint64_t todo = __ballot(real); todo;) {
+                        const int o = __builtin_amdgcn_readlane(
+                            off, __ffsll(static_cast<unsigned long long>(todo)) - 1);
+                        const bool mine = real && off == o;
+                        f32x16 y;
+#pragma unroll
+                        for (int r = 0; r < 16; r++) y[r] = mine ? dp[r] : 0.0f;
+                        add_distances(a, y, t0 + o - qb, skew, dist, far_left, far_right);
+                        todo &= ~__ballot(mine);
+                    }
+                }
+                if (CAP) {
+#pragma unroll
+                    for (int r = 0; r < 16; r++) dp[r] *= sc.f[r];
+                }
+#pragma unroll
+                for (int u = 0; u < 2; u++) {
+                    V8<T> p, d;
+                    pack(x, u, p);
+                    pack(dp, u, d);
+#pragma unroll
+                    for (int db = 0; db < DB; db++) {
+                        dv[db] = mma(Tl::cols(ot, ln, 16 * u, db), p, dv[db]);
+                        dk[db] = mma(Tl::cols(qt, ln, 16 * u, db), d, dk[db]);
+                    }
+                }
+            }
+            if (DIST) {
+                far_left = wave_sum(far_left);
+                far_right = wave_sum(far_right);
+                if (l == 0) {
+                    dist[0] += far_left;
+                    dist[width - 1] += far_right;
+                }
+                far_left = far_right = 0.0f;
+                if (kept < span) {
+                    flush(h, dists, begun);
+                    for (int d = l; d < width; d += kWave) dists[d] = 0.0f;
+                }
+            }
+        }
+        begun = true;
+        for (uint64_t todo = __ballot(bad && real && half == 0); todo; todo &= todo - 1) {
+            const int r = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+            const Seq s = seq_of(a, __builtin_amdgcn_readlane(b, r), -1);
+            row_dkv<T>(a, g, s, t0 + r - int(s.k0), h0, span);
+            nan_seen = true;
+        }
+        if (!real || bad) continue;
+        if (g.part) {
+            float *kr = g.part + (h0 * g.total_k + t) * a.dim;
+            float *vr = kr + int64_t(a.heads) * g.total_k * a.dim;
+#pragma unroll
+            for (int db = 0; db < DB; db++) {
+                store_block(kr, dk[db], deriv_scale(a), db, a.dim);
+                store_block(vr, dv[db], 1.0f, db, a.dim);
+            }
+        } else {
+            T *kr = static_cast<T *>(g.dk.data) + t * g.dk.token_stride + kvh * g.dk.head_stride;
+            T *vr = static_cast<T *>(g.dv.data) + t * g.dv.token_stride + kvh * g.dv.head_stride;
+#pragma unroll
+            for (int db = 0; db < DB; db++) {
+                store_block(kr, dk[db], deriv_scale(a), db, a.dim);
+                store_block(vr, dv[db], 1.0f, db, a.dim);
+            }
+        }
+    }
+    if (!DIST) return;
+    for (int hg = 0; hg < span; hg++) {
+        float *p = dists + (kept > 1 ? hg : 0) * width;
+        if (nan_seen) p[a.reach] = __builtin_nanf("");
+        flush(h0 + hg, p, kept < span && begun);
+    }
+}
+
 // The gradients of keys and values from their parts, over the heads that share
 // a key head, in order: a lane has 4 elements.
 template <class T>
@@ -710,6 +1031,7 @@ __global__ __launch_bounds__(kBlock) void k_bias_buckets(Args a, const float *pa
 struct Plan {
     int q_waves, q_turns;  // of a workgroup of k_attn_dq: NW and WS
     int k_waves, k_turns;  // of k_attn_dkv
+    bool q_pack, k_pack;   // k_pack_dq, k_pack_dkv instead
     int64_t q_slots, k_slots;
     int span, parts;  // of k_attn_dkv: heads of a workgroup, workgroups of a head
     int kept;         // heads whose sums by distance it keeps at a time
@@ -749,8 +1071,12 @@ Plan plan_of(const tc_attn &a) {
     p.q_waves = p.q_turns > 1 || a.max_q <= 32 || a.total_q / n <= 64 ? 1 : 4;
     p.k_waves = p.k_turns > 1 || a.max_k <= 32 || a.total_k / n <= 64 ? 1 : 4;
     if (dkv_lds(a, p.k_waves, p.k_turns, 1) > kMaxLds) p.k_waves = p.k_turns = 1;
-    p.q_slots = tile_slots(a.total_q, a.num_seqs, 32 * p.q_waves);
-    p.k_slots = tile_slots(a.total_k, a.num_seqs, 32 * p.k_waves);
+    p.q_pack = p.q_waves * p.q_turns == 1 && 
+               pack_rows(a.total_q, n, a.num_heads, kPackBackward);
+    p.k_pack = p.k_waves * p.k_turns == 1 && 
+               pack_rows(a.total_k, n, a.num_heads, kPackBackward);
+    p.q_slots = p.q_pack ? (a.total_q + 31) / 32 : tile_slots(a.total_q, a.num_seqs, 32 * p.q_waves);
+    p.k_slots = p.k_pack ? (a.total_k + 31) / 32 : tile_slots(a.total_k, a.num_seqs, 32 * p.k_waves);
     p.span = p.k_slots * p.k_waves * p.k_turns * a.num_kv_heads >= 16 * cus ? group : 1;
     const int64_t most = 8 * cus * p.span / a.num_heads + 1;
     p.parts = int(p.k_slots < most ? p.k_slots : most);
@@ -798,8 +1124,12 @@ template <class T, bool CAP, int DH, bool DIST>
 void launch_dkv(const tc_attn &t, const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
     if (p.k_turns > 1)
         launch_dkv<T, CAP, DH, 1, 4, DIST>(t, a, p, g, stream);
-    else if (p.k_waves == 1)
+    else if (p.k_waves == 1 && !p.k_pack)
         launch_dkv<T, CAP, DH, 1, 1, DIST>(t, a, p, g, stream);
+    else if (p.k_waves == 1)
+        hipLaunchKernelGGL((k_pack_dkv<T, CAP, DH, DIST>), dim3(a.heads / p.span, p.parts),
+                           dim3(kWave), dkv_lds(t, 1, 1, p.kept), stream, a, g, int(p.k_slots),
+                           p.span, p.kept);
     else
         launch_dkv<T, CAP, DH, 4, 1, DIST>(t, a, p, g, stream);
 }
@@ -817,8 +1147,14 @@ void launch(const tc_attn &t, const Args &a, const Plan &p, const Grads &g, hipS
     if (t.total_q > 0) {
         if (p.q_turns > 1)
             launch_dq<T, CAP, DH, 1, 4, 32, 1>(a, p, g, stream);
-        else if (p.q_waves == 1)
+        else if (p.q_waves == 1 && !p.q_pack)
             launch_dq<T, CAP, DH, 1, 1, 32, 1>(a, p, g, stream);
+        else if (p.q_waves == 1)
+            hipLaunchKernelGGL((k_pack_dq<T, CAP, DH>), dim3(unsigned(p.q_slots * a.heads)),
+                               dim3(kWave),
+                               2 * 32 * DH * sizeof(T) +
+                                   (a.table ? bias_entries(a.reach) * sizeof(float) : 0),
+                               stream, a, g);
         else
             launch_dq<T, CAP, DH, 4, 1, sizeof(T) == 4 ? 32 : 64, 2>(a, p, g, stream);
     }

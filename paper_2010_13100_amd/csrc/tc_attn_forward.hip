@@ -247,6 +247,118 @@ __global__ __launch_bounds__(NW * 64, tile_waves<T>(DH, NW)) void k_attn_tile(
     }
 }
 
+// Attention of 32 queries of short sequences, side by side; a wavefront each.
+template <class T, bool CAP, int DH>
+__global__ __launch_bounds__(kWave, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_pack(
+    Args a, Source src, tc_rows q, Output<T> o) {
+    typedef Tile<T, DH> Tl;
+    const typename Tl::Lane ln = Tl::lane();
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int sh[kWave];
+    T *kt = reinterpret_cast<T *>(lds), *vt = kt + 32 * DH;
+    float *bias = reinterpret_cast<float *>(vt + 32 * DH);
+    const int id = blockIdx.x, l = threadIdx.x, half = l >> 5;
+    const int kvh = id % a.kv_heads, h = kvh * a.group + (id / a.kv_heads) % a.group;
+    const int t0 = id / a.heads * 32, last = int(a.total_q) - 1;
+    const int t = min(t0 + (l & 31), last);
+    const int b = seq_of_lane(a.q_off, a.num_seqs, t, sh);
+    int lo, hi, pos;  // keys that this lane's query sees, and its place among them
+    {
+        const Seq s = seq_of(a, b, -1);
+        const int i = t - int(s.q0);
+        lo = int(s.k0);
+        hi = lo + limit(a, s, i);
+        pos = lo + i + s.shift;
+    }
+    const int begin = __builtin_amdgcn_readlane(lo, 0), end = __builtin_amdgcn_readlane(hi, 31);
+    const int lo_max = __builtin_amdgcn_readlane(lo, 31), hi_min = __builtin_amdgcn_readlane(hi, 0);
+    Seq all{};
+    const auto kv = KvOf<T, false>::make(src, all, kvh);
+    Stage<T, T, DH, kWave, 32> st;
+    st.init(l, a.dim);
+    if (begin < end) st.load(kv, begin, end, a.dim);
+
+    V8<T> qf[DH / 16];
+    const T *qp = static_cast<const T *>(q.data) + t * q.token_stride + h * q.head_stride;
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ks++) qf[ks] = chunk_of(qp, 2 * ks + half, a.dim);
+    if (a.table) load_bias(a, h, wave_min(lo - pos), -wave_min(pos + 1 - hi), bias);
+
+    f32x16 acc[DH / 32];
+#pragma unroll
+    for (int db = 0; db < DH / 32; db++) acc[db] = zero16();
+    Softmax sm;
+    bool bad = false;  // this lane's query sees a value that was cleaned
+    for (int kb = begin; kb < end; kb += 32) {
+        const bool part = kb < lo_max || kb + 32 > hi_min;  // some rows see less of the tile
+        __builtin_amdgcn_wave_barrier();
+        st.put(kt, vt);
+        __builtin_amdgcn_wave_barrier();
+        if (part) {
+            bool any = false;
+#pragma unroll
+            for (int n = 0; n < st.IT; n++) any |= not_finite(st.b[n].x);
+            if (__any(any))
+                bad |= meets(clean_mask<T, DH>(vt, reinterpret_cast<uint32_t *>(sh)), kb, lo, hi);
+        }
+        if (kb + 32 < end) st.load(kv, kb + 32, end, a.dim);
+        f32x16 x = zero16();
+#pragma unroll
+        for (int ks = 0; ks < DH / 16; ks++) x = mma(Tl::rows(kt, ln, 0, ks), qf[ks], x);
+        float c0 = -sm.ref;
+        const bool near = a.table && __any(kb + 31 - pos > -a.reach && kb - pos < a.reach);
+        if (a.table && !near) c0 += bias[kb < pos ? 0 : 2 * (a.reach + kBiasPad)];
+        to_scores<CAP>(a, c0, x);
+        if (near) add_bias_at(a, bias, kb, pos, x);
+        if (part) {
+            apart();
+            const int from = lo - kb - 4 * half, to = hi - kb - 4 * half;
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                x[r] = reg_row(r) >= from && reg_row(r) < to ? x[r] : -INFINITY;
+        }
+        float top = x[0];
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) top = max3(top, x[r], x[r + 1]);
+        float d, keep;
+        if (sm.moves(top, d, keep)) {
+#pragma unroll
+            for (int db = 0; db < DH / 32; db++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) acc[db][r] *= keep;
+#pragma unroll
+            for (int r = 0; r < 16; r++) x[r] -= d;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            x[r] = exp2_fast(x[r]);
+            sm.sum += x[r];
+        }
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            V8<T> p;
+            pack(x, u, p);
+#pragma unroll
+            for (int db = 0; db < DH / 32; db++)
+                acc[db] = mma(Tl::cols(vt, ln, 16 * u, db), p, acc[db]);
+        }
+    }
+    sm.finish();
+    for (uint64_t todo = __ballot(bad && half == 0); todo; todo &= todo - 1) {
+        const int r = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+        const Seq s = seq_of(a, __builtin_amdgcn_readlane(b, r), -1);
+        const Split none{};
+        if (t0 + r <= last)
+            finish_row(a, s, KvOf<T, false>::make(src, s, kvh), q, o, none, h, t0 + r - int(s.q0), 0, 0);
+    }
+    if (t0 + (l & 31) > last || bad) return;
+    const float inv = inverse(sm.sum);
+    T *op = static_cast<T *>(o.out.data) + t * o.out.token_stride + h * o.out.head_stride;
+#pragma unroll
+    for (int db = 0; db < DH / 32; db++) store_block(op, acc[db], inv, db, a.dim);
+    if (o.lse && half == 0) o.lse[h * a.total_q + t] = log_sum(sm.ref, sm.sum);
+}
+
 // Attention of a few queries over many keys (decoding): the queries of all
 // heads that share a key head are the 32 columns of one block, row r being
 // query r / group, head r % group. Each wavefront takes every fourth block of
@@ -539,12 +651,13 @@ __global__ __launch_bounds__(kBlock) void k_attn_join_many(Args a, Source src, O
 struct Plan {
     bool few;
     int waves;      // of a workgroup of k_attn_tile
+    bool pack;      // k_attn_pack instead
     int row_tiles;  // of k_attn_few
     int64_t blocks;
     int chunk, splits;
 };
 
-Plan plan_of(const tc_attn &a) {
+Plan plan_of(const tc_attn &a, bool paged) {
     Plan p{};
     const int group = a.num_heads / a.num_kv_heads;
     const int64_t rows = int64_t(a.max_q) * group;
@@ -558,11 +671,14 @@ Plan plan_of(const tc_attn &a) {
             (a.max_k > 32 && few <= (rows <= 32 ? 4 * cus : cus));
     const int64_t mean = a.num_seqs ? a.total_q / a.num_seqs : 0;
     p.waves = a.max_q <= 32 || mean <= 64 ? 1 : 4;
-    p.blocks = p.few ? int64_t(a.num_seqs) * a.num_kv_heads * p.row_tiles
+    p.pack = !p.few && p.waves == 1 && !paged && 
+             pack_rows(a.total_q, a.num_seqs, a.num_heads, kPackForward);
+    p.blocks = p.pack ? (a.total_q + 31) / 32 * a.num_heads
+               : p.few ? int64_t(a.num_seqs) * a.num_kv_heads * p.row_tiles
                      : tile_slots(a.total_q, a.num_seqs, 32 * p.waves) * a.num_heads;
     p.splits = 1;
     const int64_t want = int64_t(device_cus()) * 16;
-    if (p.blocks > 0 && p.blocks < want && a.max_k > 512) {
+    if (!p.pack && p.blocks > 0 && p.blocks < want && a.max_k > 512) {
         int64_t chunk = p.few ? 512 : 256;
         while (p.blocks * ((a.max_k + chunk - 1) / chunk) > want ||
                (a.max_k + chunk - 1) / chunk > kManySplits)
@@ -592,10 +708,14 @@ void launch_tile(const Args &a, const Plan &p, const Source &src, tc_rows q, con
     const dim3 grid(unsigned(p.blocks), p.splits);
     const size_t bias = a.table ? bias_entries(a.reach) * sizeof(float) : 0;
     const int slots = int(p.blocks / a.heads);
-    if (p.waves == 1)
-        hipLaunchKernelGGL((k_attn_tile<T, CT, PAGED, CAP, DH, 1, 32, 1>), grid, dim3(64),
-                           2 * 32 * DH * sizeof(T) + bias, stream, a, src, q, o, sp, slots);
-    else
+    if (p.waves == 1) {
+        const size_t bytes = 2 * 32 * DH * sizeof(T) + bias;
+        if (!p.pack)
+            hipLaunchKernelGGL((k_attn_tile<T, CT, PAGED, CAP, DH, 1, 32, 1>), grid, dim3(64),
+                               bytes, stream, a, src, q, o, sp, slots);
+        else if constexpr (!PAGED)
+            hipLaunchKernelGGL((k_attn_pack<T, CAP, DH>), grid, dim3(64), bytes, stream, a, src, q, o);
+    } else
         hipLaunchKernelGGL((k_attn_tile<T, CT, PAGED, CAP, DH, 4, BN, 2>), grid, dim3(256),
                            4 * BN * DH * sizeof(T) + bias, stream, a, src, q, o, sp, slots);
 }
@@ -625,7 +745,7 @@ void launch(const tc_attn &t, const Args &a, const Plan &p, const Source &src, t
 tc_status forward(const char *fn, const tc_attn &t, const Source &src, int32_t cache_type,
                   tc_rows q, tc_rows out, float *lse, void *workspace,
                   size_t workspace_bytes, hipStream_t stream) {
-    const Plan p = plan_of(t);
+    const Plan p = plan_of(t, src.paged);
     size_t ml_at = 0;
     const size_t need = split_bytes(t, p, &ml_at);
     TC_REQUIRE(need == 0 || (workspace && workspace_bytes >= need &&
@@ -714,12 +834,11 @@ using namespace tc;
 using namespace tc::attn;
 
 extern "C" size_t tc_attn_workspace_bytes(const tc_attn *a, int32_t paged) {
-    (void)paged;
     if (!a || a->num_seqs <= 0 || a->total_q <= 0 || a->max_q <= 0 || a->max_k <= 0 ||
         a->num_kv_heads <= 0 || a->num_heads < a->num_kv_heads || a->head_dim <= 0)
         return 0;
     size_t ml_at = 0;
-    return split_bytes(*a, plan_of(*a), &ml_at);
+    return split_bytes(*a, plan_of(*a, paged), &ml_at);
 }
 
 extern "C" tc_status tc_attn_forward(const tc_attn *a, tc_rows q, tc_rows k, tc_rows v, tc_rows out,

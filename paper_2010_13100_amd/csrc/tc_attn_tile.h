@@ -387,6 +387,24 @@ struct Stage {
     }
 };
 
+// Whether the 8 elements hold a NaN or an infinity.
+__device__ __forceinline__ bool not_finite(const Raw<float> &r) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        m = max(m, __builtin_bit_cast(uint32_t, float(r.x[i])) & 0x7fffffffu);
+    return m >= 0x7f800000u;
+}
+__device__ __forceinline__ bool not_finite(const Raw<bf16> &r) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const u32x4 w = __builtin_bit_cast(u32x4, r.x);
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    return m[0] >= 0x7f80 || m[1] >= 0x7f80;
+}
+
 // Sets what is not finite in this thread's part of a tile of ROWS rows to zero
 // and calls each(row) for every such row. Between two barriers.
 template <class T, int DH, int NT, int ROWS, class Each>
@@ -465,6 +483,57 @@ __device__ __forceinline__ int seq_of_slot(const int32_t *off, int num_seqs, int
     return b;
 }
 
+// --- rows of short sequences side by side ----------------------------------------
+//
+// Where sequences are shorter than a tile, a wavefront takes 32 rows of the whole
+// batch in order, of however many sequences: each lane has its own sequence, and
+// its row sees the columns [lo, hi) of the whole batch. lo and hi grow with the
+// row, so that lanes 0 and 31 hold their extremes.
+
+// The sequence of this lane's row t (uniform search for lane 0's, then a walk
+// over the offsets that follow, 64 at a time). sh: 64 ints of LDS.
+__device__ __forceinline__ int seq_of_lane(const int32_t *off, int num_seqs, int t, int *sh) {
+    const int l = threadIdx.x & 63;
+    const int first = __builtin_amdgcn_readfirstlane(t);
+    int b = last_at_most(num_seqs, first, [&](int n) { return int64_t(off[n]); });
+    for (int c = b + 1;; c += kWave) {
+        sh[l] = c + l < num_seqs ? off[c + l] : INT32_MAX;
+        __builtin_amdgcn_wave_barrier();
+        int n = 0;  // of the 64, those that do not pass t
+#pragma unroll
+        for (int step = 32; step > 0; step >>= 1) n += sh[n + step - 1] <= t ? step : 0;
+        n += sh[n] <= t ? 1 : 0;
+        __builtin_amdgcn_wave_barrier();
+        b += n;
+        if (!__any(n == kWave)) return b;
+    }
+}
+
+// Finds the rows r of a tile that clean_tile cleans, as a mask (whole wavefront).
+template <class T, int DH>
+__device__ __forceinline__ uint32_t clean_mask(T *t, uint32_t *sh) {
+    const int l = threadIdx.x & 63;
+    if (l == 0) *sh = 0;
+    __builtin_amdgcn_wave_barrier();
+    clean_tile<T, DH, kWave, 32>(t, l, [&](int r) { atomicOr(sh, uint32_t(1) << r); });
+    __builtin_amdgcn_wave_barrier();
+    return *reinterpret_cast<volatile uint32_t *>(sh);
+}
+
+// Whether a tile's rows from `at` on that are in `mask` meet [lo, hi).
+__device__ __forceinline__ bool meets(uint32_t mask, int at, int lo, int hi) {
+    const int from = min(max(lo - at, 0), 32), to = min(max(hi - at, 0), 32);
+    if (from >= to) return false;
+    const uint32_t upto = to == 32 ? ~0u : (1u << to) - 1;
+    return (mask & upto & (~0u << from)) != 0;
+}
+
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o, kWave));
+    return x;
+}
+
 // --- the distance bias in LDS ---------------------------------------------------
 //
 // Entry i is the bias (times log2 e) of distance i - reach - 63, cut to the
@@ -509,6 +578,26 @@ __device__ __forceinline__ void add_bias_queries(const Args &a, const float *lds
     const float *p = lds + (rel - 4 * (l >> 5) + (l & 31) + a.reach + kBiasPad);
 #pragma unroll
     for (int r = 0; r < 16; r++) x[r] += p[-reg_row(r)];
+}
+
+// Adds the bias to a block whose row 0 is key k0 and whose column is at position
+// `pos` (keys as rows), or whose row 0 is query q0 and whose column is a key at
+// kpos (queries as rows): positions that differ from lane to lane. Where the
+// entries would begin outside of the table, the row's are all past the reach, and
+// the table's ends hold their bias.
+__device__ __forceinline__ void add_bias_at(const Args &a, const float *lds, int k0, int pos,
+                                            f32x16 &x) {
+    const int half = (threadIdx.x & 63) >> 5, end = a.reach + kBiasPad;
+    const int d = min(max(k0 + 4 * half - pos, -end), end - 27);
+#pragma unroll
+    for (int r = 0; r < 16; r++) x[r] += lds[d + end + reg_row(r)];
+}
+__device__ __forceinline__ void add_bias_queries_at(const Args &a, const float *lds, int q0,
+                                                    int kpos, f32x16 &x) {
+    const int half = (threadIdx.x & 63) >> 5, end = a.reach + kBiasPad;
+    const int d = min(max(kpos - q0 - 4 * half, 27 - end), end);
+#pragma unroll
+    for (int r = 0; r < 16; r++) x[r] += lds[d + end - reg_row(r)];
 }
 
 // Products to scores, plus c0.
@@ -559,14 +648,15 @@ struct Softmax {
     float ref = 0.0f, sum = 0.0f;
     bool fresh = true;  // no key seen
     // For a block's scores minus ref with maximum `top` in this half: true if
-    // some row's ref moves; then all scores go down by d, sums are times keep.
+    // some row's ref moves; then all scores go down by d, sums are times keep (0
+    // and 1 in rows that stay: no row's bits depend on another's).
     __device__ __forceinline__ bool moves(float top, float &d, float &keep) {
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        if (!__any(top > 8.0f || (fresh && top > -INFINITY))) return false;
-        const bool seen = top > -INFINITY;
-        d = fresh ? (seen ? top : 0.0f) : fmaxf(top, 0.0f);
+        const bool mine = top > 8.0f || (fresh && top > -INFINITY);
+        if (!__any(mine)) return false;
+        d = mine ? top : 0.0f;
         keep = exp2_fast(-d);
-        fresh = fresh && !seen;
+        fresh = fresh && !mine;
         ref += d;
         sum *= keep;
         return true;

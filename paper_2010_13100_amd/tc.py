@@ -282,20 +282,25 @@ def tc_embed_coalesce(expanded, num_pairs, seg_offsets, sorted_pos, num_unique, 
         "tc_embed_coalesce")
 
 
+_NO_ROWS = TcRows(None, 0, 0)
+
+
 def _rows(t: torch.Tensor | None, dtype, name, heads, dim) -> TcRows:
     """tc_rows of a [tokens, heads, dim] tensor whose last dimension is contiguous."""
     if t is None:
-        return TcRows(None, 0, 0)
+        return _NO_ROWS
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError(f"{name} must be [tokens, {heads}, {dim}], got {list(t.shape)}")
-    st = t.stride()
-    if st[2] != 1:
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"{name} must be [tokens, {heads}, {dim}], got {list(shape)}")
+    token, head, elem = t.stride()
+    if elem != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return TcRows(t.data_ptr(), st[0] if t.shape[0] > 1 else 0, st[1] if heads > 1 else 0)
+    # strides of dimensions of one entry mean nothing
+    return TcRows(t.data_ptr(), token if shape[0] > 1 else 0, head if heads > 1 else 0)
 
 
 def _same_tokens(what, first, *others):
@@ -370,7 +375,9 @@ def _cache_rows(fn, name, cache, num_seqs, offsets, k, v, stream):
 
 def _sized(t, dtype, name, numel):
     """_ptr of a tensor that holds at least `numel` elements."""
-    if t is not None and t.numel() < numel:
+    if t is None:
+        return None
+    if t.numel() < numel:
         raise ValueError(f"{name} holds {t.numel()} elements, needs {numel}")
     return _ptr(t, dtype, name)
 
@@ -432,6 +439,7 @@ class PagedCache:
             if e is not None and (e.dtype != torch.uint8 or e.shape != k.shape[:3]):
                 raise ValueError("cache: exponents must be uint8 [pages, page_size, heads]")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self._struct = None
 
     @classmethod
     def empty(cls, num_pages, page_size, num_kv_heads, head_dim, dtype=torch.float8_e4m3fn,
@@ -443,16 +451,24 @@ class PagedCache:
                    torch.empty(shape, dtype=dtype, device=device), *exps)
 
     def struct(self, page_table, lens) -> TcCache:
-        k = self.k
-        if not k.is_cuda or not self.v.is_cuda:
-            raise ValueError("cache must be on the GPU")
-        if page_table.dim() != 2 or page_table.shape[0] != lens.numel():
+        c = self._struct
+        if c is None:  # what does not change from call to call
+            k = self.k
+            if not k.is_cuda or not self.v.is_cuda:
+                raise ValueError("cache must be on the GPU")
+            c = self._struct = TcCache(
+                DTYPES[k.dtype], k.shape[1], k.shape[2], k.shape[3], k.data_ptr(),
+                self.v.data_ptr(), _ptr(self.k_exp, torch.uint8, "k_exp"),
+                _ptr(self.v_exp, torch.uint8, "v_exp"), k.stride(0), k.stride(1), k.stride(2),
+                None, 0, None)
+        # a copy: calls may overlap, the interpreter's lock is not held in them
+        c = TcCache.from_buffer_copy(c)
+        shape = page_table.shape
+        if len(shape) != 2 or shape[0] != lens.numel():
             raise ValueError("page_table must be [num_seqs, max_pages], lens [num_seqs]")
-        return TcCache(DTYPES[k.dtype], k.shape[1], k.shape[2], k.shape[3], k.data_ptr(),
-                       self.v.data_ptr(), _ptr(self.k_exp, torch.uint8, "k_exp"),
-                       _ptr(self.v_exp, torch.uint8, "v_exp"), k.stride(0), k.stride(1),
-                       k.stride(2), _ptr(page_table, torch.int32, "page_table"),
-                       page_table.shape[1], _ptr(lens, torch.int32, "lens"))
+        c.page_table, c.max_pages = _ptr(page_table, torch.int32, "page_table"), shape[1]
+        c.lens = _ptr(lens, torch.int32, "lens")
+        return c
 
     def write(self, k, v, offsets, page_table, lens, stream=None):
         """Appends the rows k, v ([tokens, heads, dim]) of every sequence to

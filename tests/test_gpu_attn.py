@@ -293,3 +293,66 @@ def test_offsets_past_2_31_elements():
     p = R.Problem([90], [90], heads, heads, dim, causal=True)
     close(a.out, R.attention(p, q, big[-90:], big[-90:])["out"], BF16, "out")
     assert sum(lens) == n
+
+
+# Batches that fill the chip, so that every kernel's own form is taken: tiles of
+# 128 rows (long sequences) and 32 rows of several short sequences side by side.
+MANY = [
+    dict(q_lens=[700] * 8, heads=8, kv=4, dim=128, causal=True, cap=20.0, buckets=32, reach=128),
+    dict(q_lens=[333, 900, 77, 650, 1000, 129], heads=12, kv=12, dim=64, buckets=16, reach=60,
+         causal=True, prefix=[100, 0, 77, 300, 999, 5]),
+    dict(q_lens=[500] * 4, k_lens=[300, 800, 500, 257], heads=16, kv=4, dim=72, causal=True),
+    dict(q_lens=[(i * 13) % 61 for i in range(900)], heads=4, kv=2, dim=64, causal=True, buckets=32,
+         reach=128, cap=6.0),
+    dict(q_lens=[1 + i % 3 for i in range(6000)], heads=3, kv=3, dim=40, buckets=9, reach=4),
+    # cross lengths: every sequence's keys are offset differently from its queries
+    dict(q_lens=[(i * 7) % 50 for i in range(900)], k_lens=[(i * 11) % 43 for i in range(900)],
+         heads=4, kv=4, dim=128, causal=True, buckets=12, reach=20),
+    dict(q_lens=[(i * 7) % 40 for i in range(1200)], k_lens=[(i * 11) % 90 for i in range(1200)],
+         heads=2, kv=1, dim=64, buckets=12, reach=20, causal=True,
+         prefix=[(i * 5) % 60 for i in range(1200)]),
+    # a wide reach with shared heads: sums by distance of one head at a time
+    dict(q_lens=[60] * 1100, heads=8, kv=2, dim=64, causal=True, buckets=40, reach=1024),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", range(len(MANY)))
+def test_full_chip(n, dtype):
+    print(f"\n[attn] many {n} {dtype}", flush=True)
+    check(*make(dtype=dtype, seed=20 + n, **MANY[n]), dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[37] * 1000, [600] * 8], ids=["short", "long"])
+def test_masked_values_do_not_enter_full_chip(lens, dtype):
+    """As above where the chip is full: sequences beside a bad one, and rows
+    before a bad key, keep their bits."""
+    heads = 2 if lens[0] < 100 else 8
+    p, a, x, off = make(lens, heads=heads, kv=heads // 2, dim=64, dtype=dtype, causal=True, buckets=8,
+                        reach=9)
+    run(p, a, x, off)
+    keep = {s: getattr(a, s).clone() for s in ("out", "lse", "dq", "dk", "dv")}
+    n, at = lens[0], lens[0] // 2  # sequence 3, keys from `at` on
+    first, end = 3 * n, 4 * n
+    y = {s: t.clone() for s, t in x.items()}
+    for s in ("k", "v"):
+        y[s][first + at:end] = float("nan")
+    run(p, a, y, off)
+    same = torch.ones(sum(lens), dtype=torch.bool, device="cuda")
+    same[first + at:end] = False
+    for s in ("out", "dq"):
+        assert torch.equal(getattr(a, s)[same], keep[s][same]), s
+    assert torch.equal(a.lse[:, same], keep["lse"][:, same])
+    assert torch.isnan(a.out[~same].float()).any(-1).all()
+    same[first:end] = False
+    for s in ("dk", "dv"):
+        assert torch.equal(getattr(a, s)[same], keep[s][same]), s
+    y = {s: t.clone() for s, t in x.items()}
+    y["q"][first:first + at] = float("inf")
+    y["dout"][first:first + at] = float("nan")
+    run(p, a, y, off)
+    same[:] = True
+    same[first:first + at] = False
+    for s in ("out", "dq", "dk", "dv"):
+        assert torch.equal(getattr(a, s)[same], keep[s][same]), s
