@@ -72,14 +72,16 @@ __device__ void finish_row(const Args &a, const Seq &s, const KV &kv, tc_rows q,
 // tiles of 32 keys, 803 with two and tiles of 64, 895 with two and a branch-free
 // path for the tiles that need no mask or bias (more registers). Heads of 64
 // take 526 us with tiles of 64 and no cut, 571 to 584 with three to five.
+// Pages cost address arithmetic for every row of a tile, and tiles of 64 are
+// better for wide heads too: 8 x 512 queries over up to 16384 keys, 160 us and 198.
 template <class T>
-constexpr int tile_waves(int dh, int nw) {
-    if (sizeof(T) == 2 && dh > 64 && nw > 1) return 3;
+constexpr int tile_waves(int dh, int nw, bool paged) {
+    if (sizeof(T) == 2 && dh > 64 && nw > 1 && !paged) return 3;
     return sizeof(T) * dh <= 256 ? 2 : 1;
 }
 template <class T>
-constexpr int tile_keys(int dh) {
-    return sizeof(T) == 2 && dh <= 64 ? 64 : 32;
+constexpr int tile_keys(int dh, bool paged) {
+    return sizeof(T) == 2 && (dh <= 64 || paged) ? 64 : 32;
 }
 
 // Attention of NW*32 queries of one head: a wavefront has 32 queries, the
@@ -87,7 +89,7 @@ constexpr int tile_keys(int dh) {
 // tile arrives while this one is worked on; a lone wavefront, whose share of a
 // tile is four times as large, has no registers for that.
 template <class T, class CT, bool PAGED, bool CAP, int DH, int NW, int BN, int NBUF>
-__global__ __launch_bounds__(NW * 64, tile_waves<T>(DH, NW)) void k_attn_tile(
+__global__ __launch_bounds__(NW * 64, tile_waves<T>(DH, NW, PAGED)) void k_attn_tile(
     Args a, Source src, tc_rows q, Output<T> o, Split sp, int slots) {
     typedef Tile<T, DH> Tl;
     const typename Tl::Lane ln = Tl::lane();
@@ -390,6 +392,15 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
     const int end = sp.chunk ? min(seen, j0 + sp.chunk) : seen;
     const int seen_first = limit(a, s, i_first);
     const auto kv = KvOf<CT, PAGED>::make(src, s, kvh);
+
+    // the first block's loads before all others: they take the longest
+    constexpr int STEP = 32 * NW;
+    Stage<T, CT, DH, 64, 32> st;
+    st.init(l, a.dim);
+    int kb = j0 + wave * 32;
+    st.look_up(kv, kb, end);
+    if (kb < end) st.load(kv, kb, end, a.dim);
+    st.look_up(kv, kb + STEP, end);
     if (threadIdx.x == 0) first_bad = INT32_MAX;
     __syncthreads();
 
@@ -409,13 +420,6 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
     for (int db = 0; db < DB; db++) acc[db] = zero16();
     Softmax sm;
 
-    constexpr int STEP = 32 * NW;
-    Stage<T, CT, DH, 64, 32> st;
-    st.init(l, a.dim);
-    int kb = j0 + wave * 32;
-    st.look_up(kv, kb, end);
-    if (kb < end) st.load(kv, kb, end, a.dim);
-    st.look_up(kv, kb + STEP, end);
     for (; kb < end; kb += STEP) {
         st.put(kt, vt);
         if (kb + STEP < end) {
@@ -704,7 +708,7 @@ size_t split_bytes(const tc_attn &a, const Plan &p, size_t *ml_at) {
 template <class T, class CT, bool PAGED, bool CAP, int DH>
 void launch_tile(const Args &a, const Plan &p, const Source &src, tc_rows q, const Output<T> &o,
                  const Split &sp, hipStream_t stream) {
-    constexpr int BN = tile_keys<T>(DH);
+    constexpr int BN = tile_keys<T>(DH, PAGED);
     const dim3 grid(unsigned(p.blocks), p.splits);
     const size_t bias = a.table ? bias_entries(a.reach) * sizeof(float) : 0;
     const int slots = int(p.blocks / a.heads);
