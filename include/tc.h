@@ -453,7 +453,7 @@ typedef struct tc_attn {
     const int32_t *q_offsets;    /* [num_seqs + 1], from 0 to total_q */
     const int32_t *k_offsets;    /* [num_seqs + 1], from 0 to total_k (not for tc_attn_paged) */
     const int32_t *prefix_lens;  /* [num_seqs], or NULL; only with causal */
-    int64_t total_q, total_k;
+    int64_t total_q, total_k;    /* (tc_attn_paged: total_k may be 0) */
     int32_t max_q, max_k;        /* upper bounds on every sequence's queries and keys */
 } tc_attn;
 
@@ -545,8 +545,9 @@ tc_status tc_cache_read(const tc_cache *c, int32_t dtype, int32_t num_seqs,
 /*
  * tc_attn_forward with keys and values from a cache that already holds the
  * queries' own rows: sequence b has lens[b] keys and its queries are the last
- * ones of them (one query per sequence: a decoding step). a->k_offsets and
- * a->total_k are not used; a->max_k bounds lens. a->dtype is the type of q
+ * ones of them (one query per sequence: a decoding step). a->k_offsets is not
+ * used; a->max_k bounds lens; a->total_k, if not 0, is the sum of lens or a guess
+ * at it, and only decides how keys are split over workgroups. a->dtype is the type of q
  * and out. The workspace is tc_attn_workspace_bytes(a, 1) bytes, 256-byte
  * aligned.
  */

@@ -361,6 +361,32 @@ __global__ __launch_bounds__(kWave, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_p
     if (o.lse && half == 0) o.lse[h * a.total_q + t] = log_sum(sm.ref, sm.sum);
 }
 
+// Writes 4 elements from d on of a key head's row r (of its queries and heads):
+// the result, or its part of the splits.
+template <class T>
+__device__ __forceinline__ void write_row(const Args &a, const Seq &s, const Output<T> &o,
+                                          const Split &sp, int kvh, int r, int split, int j0,
+                                          int bad, int d, float big, float total, f32x4 y) {
+    const int i = r / a.group, h = kvh * a.group + r % a.group;
+    const int64_t tok = s.q0 + i, row = tok * a.heads + h;
+    const int full = limit(a, s, i);
+    if (full > bad) return;  // (finish_row's)
+    if (sp.chunk == 0 || full <= sp.chunk) {
+        if (split > 0) return;
+        const float inv = inverse(total);
+        const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+        store4(static_cast<T *>(o.out.data) + tok * o.out.token_stride + h * o.out.head_stride + d, z);
+        if (o.lse && d == 0) o.lse[h * a.total_q + tok] = log_sum(big, total);
+    } else if (j0 < full) {
+        const int64_t at = split * a.total_q * a.heads + row;
+        *reinterpret_cast<f32x4 *>(sp.o + at * a.dim + d) = y;
+        if (d == 0) {
+            sp.ml[2 * at] = big;
+            sp.ml[2 * at + 1] = total;
+        }
+    }
+}
+
 // Attention of a few queries over many keys (decoding): the queries of all
 // heads that share a key head are the 32 columns of one block, row r being
 // query r / group, head r % group. Each wavefront takes every fourth block of
@@ -533,26 +559,246 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
                 total += mw == -INFINITY ? lw : lw * exp2_fast(mw - big);
                 y += *reinterpret_cast<const f32x4 *>(sums + (w * 32 + r) * HD + (c % (HD / 4)) * 4);
             }
-            const int gr = rt * 32 + r, qi = gr / a.group, qh = kvh * a.group + gr % a.group;
-            const int64_t tok = s.q0 + qi, row = tok * a.heads + qh;
-            const int full = limit(a, s, qi);
-            if (full > bad) continue;
-            if (sp.chunk == 0 || full <= sp.chunk) {
-                if (split > 0) continue;
-                const float inv = inverse(total);
-                const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
-                store4(static_cast<T *>(o.out.data) + tok * o.out.token_stride +
-                           qh * o.out.head_stride + d, z);
-                if (o.lse && d == 0) o.lse[qh * a.total_q + tok] = log_sum(big, total);
-            } else if (j0 < full) {
-                const int64_t at = split * a.total_q * a.heads + row;
-                *reinterpret_cast<f32x4 *>(sp.o + at * a.dim + d) = y;
-                if (d == 0) {
-                    sp.ml[2 * at] = big;
-                    sp.ml[2 * at + 1] = total;
-                }
-            }
+            write_row(a, s, o, sp, kvh, rt * 32 + r, split, j0, bad, d, big, total, y);
         }
+    }
+}
+
+// The same for up to 16 rows a key head, in 16x16 blocks: half the arithmetic and
+// registers a key, so that more wavefronts and loads are under way. Keys go from
+// memory to the operands directly; values through a tile of the wavefront's own.
+template <class T, class CT, bool PAGED, int DH>
+__global__ __launch_bounds__(kBlock, sizeof(T) == 4 ? (DH == 64 ? 2 : 1)
+                                  : sizeof(CT) * DH <= 128 ? 3 : 2) void k_attn_few16(
+    Args a, Source src, tc_rows q, Output<T> o, Split sp) {
+    typedef Tile<T, DH> Tl;
+    constexpr bool Q8 = sizeof(CT) == 1;
+    constexpr int KS = DH / 32, DB = DH / 16, NW = kBlock / 64, STEP = 32 * NW;
+    constexpr int LD = Q8 ? KS / 2 : KS;  // loads of a row and lane: 16 values in 8 bits, else 8
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float stat[NW][2][16];
+    __shared__ int first_bad;
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, g = l >> 4, c = l & 15;
+    T *vt = reinterpret_cast<T *>(lds) + wave * 32 * DH;
+
+    const int id = blockIdx.x, kvh = id % a.kv_heads;
+    const Seq s = seq_at<PAGED>(a, src, id / a.kv_heads);
+    const int rows = s.qn * a.group;
+    if (rows <= 0) return;
+    const int i_last = s.qn - 1;
+    const int split = blockIdx.y, j0 = split * sp.chunk;
+    const int seen = limit(a, s, i_last);
+    if (split > 0 && j0 >= seen) return;
+    const int end = sp.chunk ? min(seen, j0 + sp.chunk) : seen;
+    const int seen_first = limit(a, s, 0);
+    const auto kv = KvOf<CT, PAGED>::make(src, s, kvh);
+
+    // 8-element chunk n of this lane's part of a row, in the order of the products
+    auto chunk_at = [&](int n) { return Q8 ? (n >> 1) * 8 + 2 * g + (n & 1) : 4 * n + g; };
+    typedef typename std::conditional<Q8, u32x4, Raw<CT>>::type Data;
+    Data kr[2][LD], vr[2][LD];
+    uint32_t ke[2], ve[2];
+    int page[2];
+    const bool both = (a.dim & 8) == 0;  // 8 bits: all 16 values of a load are in the row
+    auto look_up = [&](int kb) {
+        if constexpr (PAGED)
+            if (kb < end)
+#pragma unroll
+                for (int n = 0; n < 2; n++) page[n] = kv.page(min(kb + 16 * n + c, end - 1));
+    };
+    auto load = [&](Data &d, const CT *p, int n) {
+        const int e = chunk_at(Q8 ? 2 * n : n) * 8, at = e < a.dim ? e : 0;
+        if constexpr (Q8) {
+            typedef u32x4 u32x4_8 __attribute__((aligned(8)));
+            if (both) {
+                d = *reinterpret_cast<const u32x4_8 *>(p + at);
+            } else {
+                const u32x2 x = *reinterpret_cast<const u32x2 *>(p + at);
+                const u32x2 y = *reinterpret_cast<const u32x2 *>(p + (e + 8 < a.dim ? e + 8 : 0));
+                d = u32x4{x[0], x[1], y[0], y[1]};
+            }
+        } else {
+            d = load_raw(p + at, 0);
+        }
+    };
+    auto locate = [&](int kb, int n) {
+        const int j = min(kb + 16 * n + c, end - 1);
+        if constexpr (PAGED)
+            return kv.loc(j, page[n]);
+        else
+            return kv.loc(j);
+    };
+    Loc at[2];
+    auto load_k = [&](int kb) {
+#pragma unroll
+        for (int n = 0; n < 2; n++) {
+            at[n] = locate(kb, n);
+            ke[n] = kv.k_exp(at[n]);
+#pragma unroll
+            for (int m = 0; m < LD; m++) load(kr[n][m], kv.k(at[n]), m);
+        }
+    };
+    auto load_v = [&]() {  // of the keys of the last load_k
+#pragma unroll
+        for (int n = 0; n < 2; n++) {
+            ve[n] = kv.v_exp(at[n]);
+#pragma unroll
+            for (int m = 0; m < LD; m++) load(vr[n][m], kv.v(at[n]), m);
+        }
+    };
+    auto value = [&](const Data *d, uint32_t e, int ks) {
+        V8<T> x;
+        if constexpr (Q8)
+            expand(Raw<fp8>{u32x2{d[ks >> 1][2 * (ks & 1)], d[ks >> 1][2 * (ks & 1) + 1]}, e}, x);
+        else
+            expand(d[ks], x);
+        if (a.dim < DH) {
+            apart();
+            x = chunk_at(ks) * 8 < a.dim ? x : zero8<T>();
+        }
+        return x;
+    };
+    int kb = j0 + wave * 32;
+    look_up(kb);
+    if (kb < end) {
+        load_k(kb);
+        load_v();
+    }
+    look_up(kb + STEP);
+    if (threadIdx.x == 0) first_bad = INT32_MAX;
+    __syncthreads();
+
+    const int r0 = min(c, rows - 1), i = r0 / a.group, h = kvh * a.group + r0 % a.group;
+    const int64_t t = s.q0 + i;
+    const int lim = min(limit(a, s, i), end), pos = i + s.shift;
+    V8<T> qf[KS];
+    const T *qp = static_cast<const T *>(q.data) + t * q.token_stride + h * q.head_stride;
+#pragma unroll
+    for (int ks = 0; ks < KS; ks++) qf[ks] = chunk_of(qp, chunk_at(ks), a.dim);
+    const float far_left = a.table ? log2_bias(a, h, -a.reach) : 0.0f;
+    const float far_right = a.table ? log2_bias(a, h, a.reach) : 0.0f;
+    f32x4 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; db++) acc[db] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float ref = 0.0f, sum = 0.0f;
+    bool fresh = true;
+
+    for (; kb < end; kb += STEP) {
+        const bool more = kb + STEP < end;
+        f32x4 x[2];
+#pragma unroll
+        for (int n = 0; n < 2; n++) {
+            x[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ks++) x[n] = mma16(value(kr[n], ke[n], ks), qf[ks], x[n]);
+        }
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+#pragma unroll
+            for (int ks = 0; ks < KS; ks++)
+                Tl::put(vt, 16 * n + c, chunk_at(ks), value(vr[n], ve[n], ks));
+        if (more) {
+            load_k(kb + STEP);
+            load_v();
+            look_up(kb + 2 * STEP);
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (min(kb + 32, end) > seen_first) {  // some rows see less of the block
+            clean_tile<T, DH, 64, 32>(vt, l, [&](int r) { atomicMin(&first_bad, kb + r); });
+            __builtin_amdgcn_wave_barrier();
+        }
+        // this lane's keys: kb + 16*n + 4*g + r
+        const int lo = kb - (i_last + s.shift), hi = kb + 31 - s.shift;
+        const bool near = a.table && hi > -a.reach && lo < a.reach;
+        const float c0 = a.table && !near ? (hi <= -a.reach ? far_left : far_right) - ref : -ref;
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) x[n][r] = score(a, x[n][r], c0);
+        if (near) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                y[e] = log2_bias(a, h, kb + 16 * (e >> 2) + 4 * g + (e & 3) - pos);
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[e >> 2][e & 3] += y[e];
+        }
+        if (kb + 32 > seen_first || kb + 32 > end) {
+            apart();
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (kb + 16 * (e >> 2) + 4 * g + (e & 3) >= lim) x[e >> 2][e & 3] = -INFINITY;
+        }
+        float top = max3(x[0][0], x[0][1], x[0][2]);
+        top = max3(top, x[0][3], x[1][0]);
+        top = max3(top, x[1][1], x[1][2]);
+        top = fmaxf(top, x[1][3]);
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const bool mine = top > 8.0f || (fresh && top > -INFINITY);  // as in Softmax
+        if (__any(mine)) {
+            const float d = mine ? top : 0.0f, keep = exp2_fast(-d);
+            fresh = fresh && !mine;
+            ref += d;
+            sum *= keep;
+#pragma unroll
+            for (int db = 0; db < DB; db++) acc[db] *= keep;
+#pragma unroll
+            for (int n = 0; n < 2; n++) x[n] -= d;
+        }
+        f32x16 p16;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            p16[e] = exp2_fast(x[e >> 2][e & 3]);
+            sum += p16[e];
+        }
+        V8<T> p;
+        pack(p16, 0, p);
+#pragma unroll
+        for (int db = 0; db < DB; db++) acc[db] = mma16(cols16<T, DH>(vt, db), p, acc[db]);
+        __builtin_amdgcn_wave_barrier();
+    }
+    sum += __shfl_xor(sum, 16, kWave);
+    sum += __shfl_xor(sum, 32, kWave);
+    if (sum == 0.0f) ref = -INFINITY;
+    if (g == 0) {
+        stat[wave][0][c] = ref;
+        stat[wave][1][c] = sum;
+    }
+    __syncthreads();  // the tiles become the buffers of the sums
+    const int bad = first_bad;
+    if (bad < seen)
+        for (int r = wave; r < rows; r += NW)
+            if (limit(a, s, r / a.group) > bad)
+                finish_row(a, s, kv, q, o, sp, kvh * a.group + r % a.group, r / a.group, j0, split);
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; w++) top = fmaxf(top, stat[w][0][c]);
+    const float mine = split_weight(ref, sum, top);
+    float *sums = reinterpret_cast<float *>(lds);  // [NW][16][DH]
+    if (c < rows) {
+#pragma unroll
+        for (int db = 0; db < DB; db++) {
+            const float y[4] = {acc[db][0] * mine, acc[db][1] * mine, acc[db][2] * mine,
+                                acc[db][3] * mine};
+            store4(sums + (wave * 16 + c) * DH + 16 * db + 4 * g, y);
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < rows * (DH / 4); e += kBlock) {
+        const int r = e / (DH / 4), d = (e % (DH / 4)) * 4;
+        if (d >= a.dim) continue;
+        f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+        float big = -INFINITY, total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; w++) big = fmaxf(big, stat[w][0][r]);
+#pragma unroll
+        for (int w = 0; w < NW; w++) {
+            const float mw = stat[w][0][r], lw = stat[w][1][r];
+            total += mw == -INFINITY ? lw : lw * exp2_fast(mw - big);
+            y += *reinterpret_cast<const f32x4 *>(sums + (w * 16 + r) * DH + d);
+        }
+        write_row(a, s, o, sp, kvh, r, split, j0, bad, d, big, total, y);
     }
 }
 
@@ -653,13 +899,18 @@ __global__ __launch_bounds__(kBlock) void k_attn_join_many(Args a, Source src, O
 
 // Which kernel and which splits a call takes, from its sizes alone.
 struct Plan {
-    bool few;
+    bool few, few16;
     int waves;      // of a workgroup of k_attn_tile
     bool pack;      // k_attn_pack instead
     int row_tiles;  // of k_attn_few
     int64_t blocks;
     int chunk, splits;
 };
+
+// Workgroups a CU that splits aim at. 64 sequences of 4096 keys in 8 bits, one query
+// each, take 118 us with 3, 145 with 5 and 8; 8 x 512 queries over up to 16384
+// keys by k_attn_tile 223, 160 and 249.
+constexpr int kSplitGroupsFew = 3, kSplitGroupsTile = 5;
 
 Plan plan_of(const tc_attn &a, bool paged) {
     Plan p{};
@@ -673,19 +924,24 @@ Plan plan_of(const tc_attn &a, bool paged) {
     const int64_t few = int64_t(a.num_seqs) * a.num_kv_heads * p.row_tiles, cus = device_cus();
     p.few = (rows <= 64 && a.max_k > 128) ||
             (a.max_k > 32 && few <= (rows <= 32 ? 4 * cus : cus));
-    const int64_t mean = a.num_seqs ? a.total_q / a.num_seqs : 0;
-    p.waves = a.max_q <= 32 || mean <= 64 ? 1 : 4;
+    p.few16 = p.few && rows <= 16;
+    const int64_t mean_q = a.num_seqs ? a.total_q / a.num_seqs : 0;
+    p.waves = a.max_q <= 32 || mean_q <= 64 ? 1 : 4;
     p.pack = !p.few && p.waves == 1 && !paged && 
              pack_rows(a.total_q, a.num_seqs, a.num_heads, kPackForward);
     p.blocks = p.pack ? (a.total_q + 31) / 32 * a.num_heads
                : p.few ? int64_t(a.num_seqs) * a.num_kv_heads * p.row_tiles
                      : tile_slots(a.total_q, a.num_seqs, 32 * p.waves) * a.num_heads;
     p.splits = 1;
-    const int64_t want = int64_t(device_cus()) * 16;
-    if (!p.pack && p.blocks > 0 && p.blocks < want && a.max_k > 512) {
-        int64_t chunk = p.few ? 512 : 256;
-        while (p.blocks * ((a.max_k + chunk - 1) / chunk) > want ||
-               (a.max_k + chunk - 1) / chunk > kManySplits)
+    // Keys are split so that about kSplitGroups* workgroups a CU have some. `mean`
+    // keys a sequence are known (or the most a sequence has); every second
+    // sequence's last split is taken as full.
+    const double mean = a.num_seqs > 0 && a.total_k > 0 ? double(a.total_k) / a.num_seqs : a.max_k;
+    const double want = double(cus) * (p.few ? kSplitGroupsFew : kSplitGroupsTile);
+    if (!p.pack && p.blocks > 0) {
+        int64_t chunk = 256;
+        while (chunk < a.max_k && (p.blocks * (mean / chunk + 0.5) > want ||
+                                   (a.max_k + chunk - 1) / chunk > kManySplits))
             chunk *= 2;
         const int64_t n = (a.max_k + chunk - 1) / chunk;
         if (n > 1) {
@@ -727,7 +983,11 @@ void launch_tile(const Args &a, const Plan &p, const Source &src, tc_rows q, con
 template <class T, class CT, bool PAGED, int DH>
 void launch(const tc_attn &t, const Args &a, const Plan &p, const Source &src, tc_rows q,
             const Output<T> &o, const Split &sp, hipStream_t stream) {
-    if (p.few)
+    if (p.few16)
+        hipLaunchKernelGGL((k_attn_few16<T, CT, PAGED, DH>), dim3(unsigned(p.blocks), p.splits),
+                           dim3(kBlock), 4 * DH * (sizeof(T) == 4 ? 32 * 4 : 16 * 4), stream, a, src,
+                           q, o, sp);
+    else if (p.few)
         hipLaunchKernelGGL((k_attn_few<T, CT, PAGED, DH>), dim3(unsigned(p.blocks), p.splits),
                            dim3(kBlock), 4 * 2 * 32 * DH * sizeof(T), stream, a, src, q, o, sp,
                            p.row_tiles);
@@ -795,7 +1055,7 @@ tc_status check_attn(const char *fn, const tc_attn *a, bool paged) {
     TC_REQUIRE(a->dtype == TC_F32 || a->dtype == TC_BF16, TC_ERR_INVALID_ARG,
                "%s: dtype %d is neither TC_F32 nor TC_BF16", fn, a->dtype);
     TC_REQUIRE(a->num_seqs >= 0 && a->max_q >= 0 && a->max_k >= 0 && a->total_q >= 0 &&
-                   (paged || a->total_k >= 0),
+                   a->total_k >= 0,
                TC_ERR_INVALID_ARG, "%s: negative size", fn);
     TC_REQUIRE(a->num_kv_heads >= 1 && a->num_heads >= 1 && a->num_heads <= 4096 &&
                    a->num_heads % a->num_kv_heads == 0,

@@ -44,6 +44,17 @@ __device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
     return c;
 }
 
+// 16x16 blocks, over 32 values: an operand is row l%16, values 8*(l/16) .. +7; the
+// result's register r is row 4*(l/16) + r, column l%16.
+__device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(f32x8 a, f32x8 b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
 __device__ __forceinline__ f32x16 zero16() {
     f32x16 z;
 #pragma unroll
@@ -427,6 +438,29 @@ __device__ __forceinline__ V8<T> chunk_of(const T *row, int chunk, int dim) {
     V8<T> x;
     expand(load_raw(row + (chunk * 8 < dim ? chunk * 8 : 0), 0), x);
     return chunk * 8 < dim ? x : zero8<T>();
+}
+
+// The same of two 16x16 blocks' columns: 16 columns from 16*db, as rows; the 32
+// values are rows 4*(l/16) + 0 .. 3 of the first and of the second 16 of a tile.
+template <class T, int DH>
+__device__ __forceinline__ V8<T> cols16(const T *t, int db) {
+    const int l = threadIdx.x & 63, g = l >> 4, j = l & 15;
+    V8<T> x;
+    if constexpr (sizeof(T) == 2) {
+        typedef __attribute__((address_space(3))) s16x4 lds4;
+        const int row = 4 * g + (j >> 2), d = 16 * db + (j & 3) * 4;
+        const T *p = t + Tile<T, DH>::at(row, d >> 3) + (d & 7);
+        const T *q = t + Tile<T, DH>::at(row + 16, d >> 3) + (d & 7);
+        const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p));
+        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(q));
+        x = __builtin_bit_cast(V8<T>, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+        const int d = 16 * db + j;
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            x[i] = t[Tile<T, DH>::at(4 * g + (i & 3) + (i < 4 ? 0 : 16), d >> 3) + (d & 7)];
+    }
+    return x;
 }
 
 // Writes a transposed block (rows are elements 32*db .. +31 of this lane's
