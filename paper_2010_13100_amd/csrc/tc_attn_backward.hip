@@ -1037,7 +1037,11 @@ struct Plan {
     int kept;         // heads whose sums by distance it keeps at a time
 };
 
-// Wavefronts take turns at tiles (WS > 1) up to this many 32-row tiles a CU.
+// Wavefronts take turns at tiles (WS > 1) up to this many 32-row tiles a CU, or, where
+// the longest sequence is over four times the mean and alone would hold up the
+// call, twice as many. Both sides, us, 6 to 8 heads in bf16: 24 sequences of log-uniform
+// lengths up to 2000 (5 tiles a CU) 315 with turns and 340 without, 48 of them (10 a CU)
+// 746 and 557; 4 x 1200 (4.8 a CU, even) 374 and 286.
 constexpr int kTurnsTiles = 4;
 
 constexpr size_t kMaxLds = 156 << 10;  // of 160 KB, the kernels' fixed arrays aside
@@ -1064,16 +1068,18 @@ Plan plan_of(const tc_attn &a) {
     const int group = a.num_heads / a.num_kv_heads;
     const int64_t cus = device_cus();
     // tiles of 32 rows: few enough that a wavefront each leaves the chip idle?
+    const int64_t q_most = kTurnsTiles * cus * (a.max_q > 4 * (a.total_q / n) ? 2 : 1);
+    const int64_t k_most = kTurnsTiles * cus * (a.max_k > 4 * (a.total_k / n) ? 2 : 1);
     const int64_t q32 = tile_slots(a.total_q, a.num_seqs, 32) * a.num_heads;
     const int64_t k32 = tile_slots(a.total_k, a.num_seqs, 32) * a.num_heads;
-    p.q_turns = q32 <= kTurnsTiles * cus && a.max_k > 32 ? 4 : 1;
-    p.k_turns = k32 <= kTurnsTiles * cus && a.max_q > 32 ? 4 : 1;
+    p.q_turns = q32 <= q_most && a.max_k > 32 ? 4 : 1;
+    p.k_turns = k32 <= k_most && a.max_q > 32 ? 4 : 1;
     p.q_waves = p.q_turns > 1 || a.max_q <= 32 || a.total_q / n <= 64 ? 1 : 4;
     p.k_waves = p.k_turns > 1 || a.max_k <= 32 || a.total_k / n <= 64 ? 1 : 4;
     if (dkv_lds(a, p.k_waves, p.k_turns, 1) > kMaxLds) p.k_waves = p.k_turns = 1;
-    p.q_pack = p.q_waves * p.q_turns == 1 && 
+    p.q_pack = p.q_waves * p.q_turns == 1 &&
                pack_rows(a.total_q, n, a.num_heads, kPackBackward);
-    p.k_pack = p.k_waves * p.k_turns == 1 && 
+    p.k_pack = p.k_waves * p.k_turns == 1 &&
                pack_rows(a.total_k, n, a.num_heads, kPackBackward);
     p.q_slots = p.q_pack ? (a.total_q + 31) / 32 : tile_slots(a.total_q, a.num_seqs, 32 * p.q_waves);
     p.k_slots = p.k_pack ? (a.total_k + 31) / 32 : tile_slots(a.total_k, a.num_seqs, 32 * p.k_waves);
@@ -1244,7 +1250,7 @@ extern "C" tc_status tc_attn_backward(const tc_attn *a, tc_rows q, tc_rows k, tc
             nullptr, nullptr, a->total_k};
     if (grad_bias && rq) g.bias_part = reinterpret_cast<float *>(ws + space.bias);
     if (rq && plan.span < args.group) g.part = reinterpret_cast<float *>(ws + space.part);
-    TC_REQUIRE(plan.q_slots * a->num_heads < (int64_t(1) << 31), 
+    TC_REQUIRE(plan.q_slots * a->num_heads < (int64_t(1) << 31),
                TC_ERR_INVALID_ARG, "%s: more than 2^31 workgroups", fn);
     backward(*a, plan, args, g, grad_bias, stream);
     return check_launch(fn);

@@ -14,7 +14,7 @@ using namespace attn;
 struct Split {
     float *o;   // [splits][total_q*heads][dim]
     float *ml;  // [splits][total_q*heads][2]
-    int32_t chunk;
+    int32_t chunk, splits;
 };
 
 template <class T>
@@ -123,7 +123,8 @@ __global__ __launch_bounds__(NW * 64, tile_waves<T>(DH, NW, PAGED)) void k_attn_
 
     const int w0 = i0 + wave * 32, i = w0 + (l & 31);
     const int lim = limit(a, s, min(i, s.qn - 1));
-    const int lim_first = limit(a, s, min(w0, s.qn - 1)), lim_last = limit(a, s, min(w0 + 31, s.qn - 1));
+    const int lim_first = limit(a, s, min(w0, s.qn - 1));
+    const int lim_last = limit(a, s, min(w0 + 31, s.qn - 1));
     const int block_first = limit(a, s, i0);
     if (a.table) load_bias(a, h, j0 - (i0 + BM - 1 + s.shift), end - 1 - (i0 + s.shift), bias);
     if (threadIdx.x == 0) first_bad = INT32_MAX;
@@ -393,8 +394,8 @@ __device__ __forceinline__ void write_row(const Args &a, const Seq &s, const Out
 // 32 keys for itself, with tiles of its own, so that nothing waits for another
 // wavefront before the end; the next block arrives while one is worked on.
 template <class T, class CT, bool PAGED, int DH>
-__global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_few(Args a, Source src, tc_rows q, Output<T> o,
-                                                     Split sp, int row_tiles) {
+__global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_few(
+    Args a, Source src, tc_rows q, Output<T> o, Split sp, int row_tiles) {
     typedef Tile<T, DH> Tl;
     const typename Tl::Lane ln = Tl::lane();
     constexpr int KS = DH / 16, DB = DH / 32, NW = kBlock / 64;
@@ -568,8 +569,9 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
 // registers a key, so that more wavefronts and loads are under way. Keys go from
 // memory to the operands directly; values through a tile of the wavefront's own.
 template <class T, class CT, bool PAGED, int DH>
-__global__ __launch_bounds__(kBlock, sizeof(T) == 4 ? (DH == 64 ? 2 : 1)
-                                  : sizeof(CT) * DH <= 128 ? 3 : 2) void k_attn_few16(
+__global__ __launch_bounds__(kBlock, sizeof(T) == 4          ? (DH == 64 ? 2 : 1)
+                                     : sizeof(CT) * DH <= 128 ? 3
+                                                              : 2) void k_attn_few16(
     Args a, Source src, tc_rows q, Output<T> o, Split sp) {
     typedef Tile<T, DH> Tl;
     constexpr bool Q8 = sizeof(CT) == 1;
@@ -806,7 +808,7 @@ __global__ __launch_bounds__(kBlock, sizeof(T) == 4 ? (DH == 64 ? 2 : 1)
 // (query, head).
 template <class T, bool PAGED>
 __global__ __launch_bounds__(kBlock) void k_attn_join(Args a, Source src, Output<T> o,
-                                                               Split sp) {
+                                                      Split sp) {
     const int l = threadIdx.x & 63;
     const int64_t rows = a.total_q * a.heads, row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (row >= rows) return;
@@ -816,7 +818,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(Args a, Source src, Output
     const Seq s = seq_at<PAGED>(a, src, b);
     const int lim = limit(a, s, int(t - s.q0));
     if (lim <= sp.chunk) return;
-    const int n = (lim + sp.chunk - 1) / sp.chunk;
+    const int n = min((lim + sp.chunk - 1) / sp.chunk, sp.splits);
     float top = -INFINITY;
     for (int k = l; k < n; k += kWave) top = fmaxf(top, sp.ml[2 * (k * rows + row)]);
 #pragma unroll
@@ -856,7 +858,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join_many(Args a, Source src, O
     const Seq s = seq_at<PAGED>(a, src, b);
     const int lim = limit(a, s, int(t - s.q0));
     if (lim <= sp.chunk) return;
-    const int n = (lim + sp.chunk - 1) / sp.chunk;
+    const int n = min((lim + sp.chunk - 1) / sp.chunk, sp.splits);
     float top = -INFINITY;
     for (int k = tid; k < n; k += kBlock) {
         weight[k] = sp.ml[2 * (k * rows + row)];
@@ -927,7 +929,7 @@ Plan plan_of(const tc_attn &a, bool paged) {
     p.few16 = p.few && rows <= 16;
     const int64_t mean_q = a.num_seqs ? a.total_q / a.num_seqs : 0;
     p.waves = a.max_q <= 32 || mean_q <= 64 ? 1 : 4;
-    p.pack = !p.few && p.waves == 1 && !paged && 
+    p.pack = !p.few && p.waves == 1 && !paged &&
              pack_rows(a.total_q, a.num_seqs, a.num_heads, kPackForward);
     p.blocks = p.pack ? (a.total_q + 31) / 32 * a.num_heads
                : p.few ? int64_t(a.num_seqs) * a.num_kv_heads * p.row_tiles
@@ -1025,8 +1027,11 @@ tc_status forward(const char *fn, const tc_attn &t, const Source &src, int32_t c
         sp.o = static_cast<float *>(workspace);
         sp.ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + ml_at);
         sp.chunk = p.chunk;
+        sp.splits = p.splits;
     }
-#define TC_LAUNCH(T, CT, PAGED)                                                           (t.head_dim <= 64                                                                          ? launch<T, CT, PAGED, 64>(t, a, p, src, q, {out, lse}, sp, stream)          : launch<T, CT, PAGED, 128>(t, a, p, src, q, {out, lse}, sp, stream))
+#define TC_LAUNCH(T, CT, PAGED)                                                        \
+    (t.head_dim <= 64 ? launch<T, CT, PAGED, 64>(t, a, p, src, q, {out, lse}, sp, stream) \
+                      : launch<T, CT, PAGED, 128>(t, a, p, src, q, {out, lse}, sp, stream))
     if (t.dtype == TC_F32) {
         if (!src.paged)
             TC_LAUNCH(float, float, false);
@@ -1106,7 +1111,8 @@ extern "C" size_t tc_attn_workspace_bytes(const tc_attn *a, int32_t paged) {
 }
 
 extern "C" tc_status tc_attn_forward(const tc_attn *a, tc_rows q, tc_rows k, tc_rows v, tc_rows out,
-                                     float *lse, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+                                     float *lse, void *workspace, size_t workspace_bytes,
+                                     hipStream_t stream) {
     const char *fn = "tc_attn_forward";
     clear_error();
     tc_status st = check_attn(fn, a, false);

@@ -237,8 +237,9 @@ struct Tile {
 //
 // A thread loads its share of a tile into registers while the tile before is
 // worked on, and puts it into LDS afterwards. (Loads that go to LDS by
-// themselves were slower: 1035 us against 870 for 2 x 8192 causal queries and
-// 16 heads of 128 bf16.) Loads are straight-line code: a load under a
+// themselves took as long, within 1%, at 2 x 8192 causal queries and 16 heads of
+// 128 bf16; in registers a tile can be widened and its padding set to zero
+// on the way.) Loads are straight-line code: a load under a
 // condition makes the compiler wait for the ones before it. Rows past the end
 // repeat the last one (they get weight 0), elements past head_dim the first
 // ones (and become 0 in LDS).
