@@ -132,10 +132,37 @@ __device__ __forceinline__ float half_tanh(float y) {
     return __builtin_amdgcn_rcpf(1.0f + exp2_fast(y));
 }
 
+// tanh itself, for fp32 operands: 1 - 2r errs by 2^-24 of 1, and c2 times that shows
+// in scores far below the cap (dq of short sequences with a cap of 50: 1.2e-6 off
+// instead of 3e-7). So below 1/4 it is the series, to 8e-9 of itself.
+__device__ __forceinline__ float tanh_of(float y) {
+    const float u = y * (0.5f * kLn2), w = u * u;
+    float p = __builtin_fmaf(w, 62.0f / 2835.0f, -17.0f / 315.0f);
+    p = __builtin_fmaf(w, p, 2.0f / 15.0f);
+    p = __builtin_fmaf(w, p, -1.0f / 3.0f);
+    const float large = __builtin_fmaf(-2.0f, half_tanh(y), 1.0f);
+    return __builtin_fabsf(u) < 0.25f ? __builtin_fmaf(u * w, p, u) : large;
+}
+
+// The capped score of product z of T operands, plus c0, and the score's
+// derivative by z over deriv_scale().
+template <class T>
+__device__ __forceinline__ float capped_score(const Args &a, float z, float c0, float &f) {
+    if (sizeof(T) == 4) {
+        const float t = tanh_of(a.c1 * z);
+        f = __builtin_fmaf(-0.25f * t, t, 0.25f);
+        return __builtin_fmaf(a.c2, t, c0);
+    }
+    const float r = half_tanh(a.c1 * z);
+    f = __builtin_fmaf(-r, r, r);
+    return __builtin_fmaf(-2.0f * a.c2, r, a.c2 + c0);
+}
+
 // The score of product z, plus c0.
+template <class T>
 __device__ __forceinline__ float score(const Args &a, float z, float c0) {
-    if (!a.capped) return __builtin_fmaf(z, a.c1, c0);
-    return __builtin_fmaf(-2.0f * a.c2, half_tanh(a.c1 * z), a.c2 + c0);
+    float f;
+    return a.capped ? capped_score<T>(a, z, c0, f) : __builtin_fmaf(z, a.c1, c0);
 }
 
 __device__ __forceinline__ float log2_bias(const Args &a, int h, int delta) {
@@ -338,13 +365,13 @@ struct RowState {
 };
 
 // Keys [j0, j1) of one query into st.
-template <class KV>
+template <class T, class KV>
 __device__ void row_forward(const Args &a, const KV &kv, Row2 q, int h, int pos, int j0, int j1,
                             RowState &st) {
     for (int j = j0; j < j1; j++) {
         const Loc l = kv.loc(j);
         const float z = dot(q, load_row(kv.k(l), kv.k_exp(l), a.dim));
-        const float s = score(a, z, a.table ? log2_bias(a, h, j - pos) : 0.0f);
+        const float s = score<T>(a, z, a.table ? log2_bias(a, h, j - pos) : 0.0f);
         const float m = fmaxf(st.m, s), base = m == -INFINITY ? 0.0f : m;
         const float keep = exp2_fast(st.m - base), p = exp2_fast(s - base);
         const Row2 v = load_row(kv.v(l), kv.v_exp(l), a.dim);

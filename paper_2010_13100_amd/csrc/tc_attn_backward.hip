@@ -18,15 +18,14 @@ struct Grads {
 
 // One pair (query, key): p, ds = p * (dp - delta) with respect to s, and g with
 // respect to the product.
+template <class T>
 __device__ __forceinline__ void pair_grad(const Args &a, float z, float bias, float lse2, float dp,
                                           float delta, float &p, float &ds, float &g) {
-    p = exp2_fast(score(a, z, bias) - lse2);
+    float f = 0.25f;
+    const float s = a.capped ? capped_score<T>(a, z, bias, f) : __builtin_fmaf(z, a.c1, bias);
+    p = exp2_fast(s - lse2);
     ds = p * (dp - delta);
-    g = ds * a.scale;
-    if (a.capped) {
-        const float t = half_tanh(a.c1 * z);
-        g *= 4.0f * __builtin_fmaf(-t, t, t);
-    }
+    g = ds * (4.0f * f * a.scale);
 }
 
 template <class T>
@@ -52,7 +51,7 @@ __device__ void row_dq(const Args &a, const Grads &g, const Seq &s, int i, int h
     for (int j = 0; j < n; j++) {
         const Row2 k = row_at<T>(g.k, s.k0 + j, kvh, a.dim), v = row_at<T>(g.v, s.k0 + j, kvh, a.dim);
         float p, ds, gs;
-        pair_grad(a, dot(q, k), a.table ? log2_bias(a, h, j - pos) : 0.0f, lse2, dot(go, v), delta,
+        pair_grad<T>(a, dot(q, k), a.table ? log2_bias(a, h, j - pos) : 0.0f, lse2, dot(go, v), delta,
                   p, ds, gs);
         dq.a += gs * k.a;
         dq.b += gs * k.b;
@@ -74,7 +73,7 @@ __device__ void row_dkv(const Args &a, const Grads &g, const Seq &s, int j, int 
             const int64_t t = s.q0 + i;
             const Row2 q = row_at<T>(g.q, t, h, a.dim), go = row_at<T>(g.grad_out, t, h, a.dim);
             float p, ds, gs;
-            pair_grad(a, dot(q, k), a.table ? log2_bias(a, h, j - i - s.shift) : 0.0f,
+            pair_grad<T>(a, dot(q, k), a.table ? log2_bias(a, h, j - i - s.shift) : 0.0f,
                       g.lse[h * a.total_q + t] * kLog2e, dot(go, v), g.delta[h * a.total_q + t], p,
                       ds, gs);
             dk.a += gs * q.a;
@@ -172,6 +171,22 @@ __device__ __forceinline__ float load_rows_and_delta(const Args &a, const Grads 
     return ((l & 31) >> 2 & 1) == half ? delta : other;
 }
 
+// delta of the rows whose keys are all in one block, from scores x (minus lse)
+// and products dp of it. Entries of this half in [from, to) count.
+__device__ __forceinline__ float block_delta(const f32x16 &x, const f32x16 &dp, int from, int to) {
+    float sum = 0.0f, total = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+        const bool in = reg_row(r) >= from && reg_row(r) < to;
+        const float p = in ? exp2_fast(x[r]) : 0.0f;
+        sum = in ? __builtin_fmaf(p, dp[r], sum) : sum;
+        total += p;
+    }
+    sum += __shfl_xor(sum, 32, kWave);
+    total += __shfl_xor(total, 32, kWave);
+    return sum / total;
+}
+
 // Orders what the threads that share a tile do to it.
 template <int WS>
 __device__ __forceinline__ void sync_tile() {
@@ -214,10 +229,12 @@ __device__ __forceinline__ void add_waves(float *sums, const f32x16 *x, Each eac
 // delta = sum_j p_j dp_j is <grad_out, out>, but out has been rounded, and the
 // bias gradient adds up so many terms p*(dp - delta) that cancel that this
 // shows. The terms of a row add up to 0, so what they do add up to here is
-// the error of delta: k_attn_dkv gets the sum of the two, exact to fp32. (Here
-// the uncorrected delta adds half as much to the error of dq as each of two
-// roundings does, that of p*(dp - delta) to bf16 for the product and that of dq
-// itself; the correction is known too late, and would take a fourth product.)
+// the error of delta: k_attn_dkv gets the sum of the two, exact to fp32. dq has the
+// uncorrected one, since the correction is known too late and would take a
+// fourth product and its registers; its error counts by 1 / (keys seen), so rows
+// that see up to 32 take delta from their block instead (one key: <grad_out, out>,
+// which leaves 0 to the last bit). p*(dp - delta) is rounded to bf16 for the
+// product, as dq itself is.
 //
 // Bound like k_attn_tile by the chain of products and exponentials: 4 x 4096 causal
 // queries, 8 heads of 128 bf16, capped, 0.34 ms, 600 TFLOP/s in its three products.
@@ -258,7 +275,7 @@ __global__ __launch_bounds__(NW *WS * 64, WS == 1 && sizeof(T) * DH <= 256 ? 2 :
     if (threadIdx.x == 0) first_bad = INT32_MAX;
 
     V8<T> qf[KS], of[KS];
-    const float delta = load_rows_and_delta<T, DH>(a, g, t, h, qf, of);
+    float delta = load_rows_and_delta<T, DH>(a, g, t, h, qf, of);
     float rest = 0.0f;
     const float lse2 = g.lse[h * a.total_q + t] * kLog2e;
 
@@ -287,9 +304,13 @@ __global__ __launch_bounds__(NW *WS * 64, WS == 1 && sizeof(T) * DH <= 256 ? 2 :
                 dp = mma(Tl::rows(vt, ln, 32 * n, ks), of[ks], dp);
             }
             const bool near = a.table && near_block(a, rel);
-            const Scores sc = scores_of<CAP>(a, a.table && !near ? far_bias(a, bias, rel) - lse2 : -lse2, x);
+            const Scores sc = scores_of<T, CAP>(a, a.table && !near ? far_bias(a, bias, rel) - lse2 : -lse2, x);
             x = sc.x;
             if (near) add_bias(a, bias, rel, x);
+            if (n == 0 && kb == 0 && lim_first <= 32) {
+                const float d = block_delta(x, dp, 0, lim - 4 * half);
+                delta = lim > 1 && lim <= 32 ? d : delta;
+            }
 #pragma unroll
             for (int r = 0; r < 16; r++) x[r] = exp2_fast(x[r]) * (dp[r] - delta);
             if (k0 + 32 > lim_first) {
@@ -389,7 +410,7 @@ __global__ __launch_bounds__(kWave, sizeof(T) * DH <= 256 ? 2 : 1) void k_pack_d
     if (begin < end) st.load(kv, begin, end, a.dim);
 
     V8<T> qf[KS], of[KS];
-    const float delta = load_rows_and_delta<T, DH>(a, g, t, h, qf, of);
+    float delta = load_rows_and_delta<T, DH>(a, g, t, h, qf, of);
     const float lse2 = g.lse[h * a.total_q + t] * kLog2e;
     float rest = 0.0f;
     if (a.table) load_bias(a, h, wave_min(lo - pos), -wave_min(pos + 1 - hi), bias);
@@ -419,9 +440,14 @@ __global__ __launch_bounds__(kWave, sizeof(T) * DH <= 256 ? 2 : 1) void k_pack_d
         float c0 = -lse2;
         const bool near = a.table && __any(kb + 31 - pos > -a.reach && kb - pos < a.reach);
         if (a.table && !near) c0 += bias[kb < pos ? 0 : 2 * (a.reach + kBiasPad)];
-        const Scores sc = scores_of<CAP>(a, c0, x);
+        const Scores sc = scores_of<T, CAP>(a, c0, x);
         x = sc.x;
         if (near) add_bias_at(a, bias, kb, pos, x);
+        const bool whole = lo >= kb && hi <= kb + 32 && hi - lo > 1;
+        if (__any(whole)) {
+            const float d = block_delta(x, dp, lo - kb - 4 * half, hi - kb - 4 * half);
+            delta = whole ? d : delta;
+        }
 #pragma unroll
         for (int r = 0; r < 16; r++) x[r] = exp2_fast(x[r]) * (dp[r] - delta);
         if (part) {
@@ -473,6 +499,15 @@ __global__ __launch_bounds__(kWave, sizeof(T) * DH <= 256 ? 2 : 1) void k_pack_d
 // keeps one head's and adds them to its own row in the workspace after each.
 // It has all heads that share a key head (span = group), or one (span = 1) and
 // leaves its part of the sum over them to k_attn_sum_heads.
+//
+// P and p*(dp - delta) are rounded to the elements' type where they enter the
+// products with grad_out and q, as p is in the forward; the bias gradient is
+// summed from fp32 values. Bound by latency: 4 x 4096 causal queries, 8 heads of 128 on
+// 2 key heads, bf16, capped, 0.64 ms, 430 TFLOP/s in its four products, matrix
+// instructions 17% of the time, with one wavefront a SIMD, since dk and dv take half of the
+// registers and the operands of the keys a quarter. Two, with the values in LDS,
+// spill 460 bytes a lane: forward and backward 1870 us and not 1300. The bias
+// gradient is 0.1 ms of it.
 template <class T, bool CAP, int DH, int NW, int WS, int BQ, bool DIST, int NBUF>
 __global__ __launch_bounds__(NW *WS * 64, WS == 1 && sizeof(T) * DH <= 128 ? 2 : 1) void k_attn_dkv(
     Args a, Grads g, int slots, int span, int kept) {
@@ -606,7 +641,7 @@ __global__ __launch_bounds__(NW *WS * 64, WS == 1 && sizeof(T) * DH <= 128 ? 2 :
                              VLDS ? Tl::rows(vt, ln, 0, ks) : vf[VLDS ? 0 : ks], dp);
                 }
                 const bool near = a.table && near_block(a, rel);
-                const Scores sc = scores_of<CAP>(a, a.table && !near ? far_bias(a, bias, rel) : 0.0f, x);
+                const Scores sc = scores_of<T, CAP>(a, a.table && !near ? far_bias(a, bias, rel) : 0.0f, x);
                 x = sc.x;
                 if (near) add_bias_queries(a, bias, rel, x);
 #pragma unroll
@@ -854,7 +889,7 @@ __global__ __launch_bounds__(kWave, sizeof(T) * DH <= 128 ? 2 : 1) void k_pack_d
                 float c0 = 0.0f;
                 const bool near = a.table && __any(kpos - qb > -a.reach && kpos - qb - 31 < a.reach);
                 if (a.table && !near) c0 = bias[kpos < qb ? 0 : 2 * (a.reach + kBiasPad)];
-                const Scores sc = scores_of<CAP>(a, c0, x);
+                const Scores sc = scores_of<T, CAP>(a, c0, x);
                 x = sc.x;
                 if (near) add_bias_queries_at(a, bias, qb, kpos, x);
 #pragma unroll

@@ -46,7 +46,7 @@ __device__ void finish_row(const Args &a, const Seq &s, const KV &kv, tc_rows q,
     const bool whole = sp.chunk == 0 || lim <= sp.chunk;
     RowState st{-INFINITY, 0.0f, {0.0f, 0.0f}};
     const T *qp = static_cast<const T *>(q.data) + t * q.token_stride + h * q.head_stride;
-    row_forward(a, kv, load_row(qp, 0, a.dim), h, i + s.shift, j0,
+    row_forward<T>(a, kv, load_row(qp, 0, a.dim), h, i + s.shift, j0,
                 whole ? lim : min(lim, j0 + sp.chunk), st);
     const bool first = (threadIdx.x & 63) == 0;
     if (whole) {
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(NW * 64, tile_waves<T>(DH, NW, PAGED)) void k_attn_
         for (int n = 0; n < NB; n++) {
             const int k0 = kb + 32 * n, rel = k0 - (w0 + s.shift);
             const bool near = a.table && near_block(a, rel);
-            to_scores<CAP>(a, a.table && !near ? far_bias(a, bias, rel) - sm.ref : -sm.ref, x[n]);
+            to_scores<T, CAP>(a, a.table && !near ? far_bias(a, bias, rel) - sm.ref : -sm.ref, x[n]);
             if (near) add_bias(a, bias, rel, x[n]);
             if (k0 + 32 > lim_first || k0 + 32 > end) {
                 apart();
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(kWave, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_p
         float c0 = -sm.ref;
         const bool near = a.table && __any(kb + 31 - pos > -a.reach && kb - pos < a.reach);
         if (a.table && !near) c0 += bias[kb < pos ? 0 : 2 * (a.reach + kBiasPad)];
-        to_scores<CAP>(a, c0, x);
+        to_scores<T, CAP>(a, c0, x);
         if (near) add_bias_at(a, bias, kb, pos, x);
         if (part) {
             apart();
@@ -479,9 +479,9 @@ __global__ __launch_bounds__(kBlock, sizeof(T) * DH <= 256 ? 2 : 1) void k_attn_
         const bool near = a.table && hi > -a.reach && lo < a.reach;
         const float c0 = a.table && !near ? (hi <= -a.reach ? far_left : far_right) - sm.ref : -sm.ref;
         if (a.capped)
-            to_scores<true>(a, c0, x);
+            to_scores<T, true>(a, c0, x);
         else
-            to_scores<false>(a, c0, x);
+            to_scores<T, false>(a, c0, x);
         if (near) {
             float y[16];
 #pragma unroll
@@ -730,7 +730,7 @@ __global__ __launch_bounds__(kBlock, sizeof(T) == 4          ? (DH == 64 ? 2 : 1
 #pragma unroll
         for (int n = 0; n < 2; n++)
 #pragma unroll
-            for (int r = 0; r < 4; r++) x[n][r] = score(a, x[n][r], c0);
+            for (int r = 0; r < 4; r++) x[n][r] = score<T>(a, x[n][r], c0);
         if (near) {
             float y[8];
 #pragma unroll

@@ -636,12 +636,12 @@ __device__ __forceinline__ void add_bias_queries_at(const Args &a, const float *
 }
 
 // Products to scores, plus c0.
-template <bool CAP>
+template <class T, bool CAP>
 __device__ __forceinline__ void to_scores(const Args &a, float c0, f32x16 &x) {
     if (CAP) {
-        const float f = -2.0f * a.c2, k = a.c2 + c0;
+        float f;
 #pragma unroll
-        for (int r = 0; r < 16; r++) x[r] = __builtin_fmaf(f, half_tanh(a.c1 * x[r]), k);
+        for (int r = 0; r < 16; r++) x[r] = capped_score<T>(a, x[r], c0, f);
     } else {
 #pragma unroll
         for (int r = 0; r < 16; r++) x[r] = __builtin_fmaf(x[r], a.c1, c0);
@@ -652,16 +652,15 @@ __device__ __forceinline__ void to_scores(const Args &a, float c0, f32x16 &x) {
 struct Scores {
     f32x16 x, f;
 };
-template <bool CAP>
+template <class T, bool CAP>
 __device__ __forceinline__ Scores scores_of(const Args &a, float c0, f32x16 z) {
     Scores s;
     if (CAP) {
-        const float g = -2.0f * a.c2, k = a.c2 + c0;
 #pragma unroll
         for (int r = 0; r < 16; r++) {
-            const float t = half_tanh(a.c1 * z[r]);
-            s.x[r] = __builtin_fmaf(g, t, k);
-            s.f[r] = __builtin_fmaf(-t, t, t);
+            float f;
+            s.x[r] = capped_score<T>(a, z[r], c0, f);
+            s.f[r] = f;
         }
     } else {
 #pragma unroll
