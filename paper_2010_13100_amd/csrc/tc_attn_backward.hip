@@ -1145,6 +1145,9 @@ Plan plan_of(const tc_attn &a) {
     const int64_t k32 = tile_slots(a.total_k, a.num_seqs, 32) * a.num_heads;
     p.q_turns = q32 <= q_most && a.max_k > 32 ? 4 : 1;
     p.k_turns = k32 <= k_most && a.max_q > 32 ? 4 : 1;
+    // Two where fp32 tiles of four do not fit beside the sums by distance: 8192 queries of a
+    // head of 128 2095 us, 3250 with one wavefront a workgroup; 4000 of 4 heads 2064 and 2022.
+    if (p.k_turns > 1 && a.dtype == TC_F32 && a.head_dim > 64 && a.bias_table) p.k_turns = 2;
     p.q_waves = p.q_turns > 1 || a.max_q <= 32 || a.total_q / n <= 64 ? 1 : 4;
     p.k_waves = p.k_turns > 1 || a.max_k <= 32 || a.total_k / n <= 64 ? 1 : 4;
     if (dkv_lds(a, p.k_waves, p.k_turns, 1) > kMaxLds) p.k_waves = p.k_turns = 1;
@@ -1199,8 +1202,11 @@ void launch_dkv(const tc_attn &t, const Args &a, const Plan &p, const Grads &g, 
 
 template <class T, bool CAP, int DH, bool DIST>
 void launch_dkv(const tc_attn &t, const Args &a, const Plan &p, const Grads &g, hipStream_t stream) {
-    if (p.k_turns > 1)
+    constexpr bool wide = sizeof(T) * DH > 256;
+    if (p.k_turns > 2)
         launch_dkv<T, CAP, DH, 1, 4, DIST>(t, a, p, g, stream);
+    else if (p.k_turns > 1)
+        launch_dkv<T, CAP, DH, 1, wide ? 2 : 4, DIST>(t, a, p, g, stream);
     else if (p.k_waves == 1 && !p.k_pack)
         launch_dkv<T, CAP, DH, 1, 1, DIST>(t, a, p, g, stream);
     else if (p.k_waves == 1)
