@@ -547,8 +547,8 @@ tc_status tc_cache_read(const tc_cache *c, int32_t dtype, int32_t num_seqs,
  * queries' own rows: sequence b has lens[b] keys and its queries are the last
  * ones of them (one query per sequence: a decoding step). a->k_offsets is not
  * used; a->max_k bounds lens; a->total_k, if not 0, is the sum of lens or a guess
- * at it, and only decides how keys are split over workgroups. a->dtype is the type of q
- * and out. The workspace is tc_attn_workspace_bytes(a, 1) bytes, 256-byte
+ * at it, and only decides how keys are split over workgroups. a->dtype is the
+ * type of q and out. The workspace is tc_attn_workspace_bytes(a, 1) bytes, 256-byte
  * aligned.
  */
 tc_status tc_attn_paged(const tc_attn *a, tc_rows q, const tc_cache *c, tc_rows out, float *lse,

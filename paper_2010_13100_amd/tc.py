@@ -429,7 +429,8 @@ class PagedCache:
         if k.dtype not in DTYPES or v.dtype != k.dtype:
             raise ValueError(f"cache: unsupported dtypes {k.dtype}, {v.dtype}")
         if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride():
-            raise ValueError("cache: k and v must be [pages, page_size, heads, dim], laid out alike")
+            raise ValueError("cache: k and v must be [pages, page_size, heads, dim], laid out "
+                             "alike")
         if k.stride(3) != 1:
             raise ValueError("cache: the last dimension must be contiguous")
         self.quantised = DTYPES[k.dtype] == TC_FP8
